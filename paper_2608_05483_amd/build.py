@@ -2,8 +2,9 @@
 
 Each kernel has a source file of its own (``csrc/k_*.hip``), so the device
 compiles, which take most of the time, run in parallel; the objects are then
-linked into one library with the host side (``csrc/plora.hip``) and the
-split-KV attention kernels (``csrc/attention.hip``)."""
+linked into one library with the host side (``csrc/plora.hip``), the split-KV
+attention kernels (``csrc/attention.hip``) and the operators of a step over a
+paged cache (``csrc/paged/``)."""
 from __future__ import annotations
 
 import glob
@@ -16,7 +17,8 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 SRCS = sorted(glob.glob(os.path.join(CSRC, "k_*.hip"))) + [
-    os.path.join(CSRC, "plora.hip"), os.path.join(CSRC, "attention.hip")]
+    os.path.join(CSRC, "plora.hip"), os.path.join(CSRC, "attention.hip")] + sorted(
+        glob.glob(os.path.join(CSRC, "paged", "*.hip")))
 PROBE_SRC = os.path.join(CSRC, "read_ceiling.hip")
 HEADER = os.path.join(ROOT, "include", "plora.h")
 LIB = os.path.join(PKG, "libplora.so")
@@ -29,7 +31,8 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = ["--offload-arch=gfx950", "-Xclang", "-target-feature", "-Xclang",
         "-packed-fp32-ops"]
 CFLAGS = [*ARCH, "-O3", "-std=c++17", "-fPIC", "-Wall", "-I",
-          os.path.join(ROOT, "include"), "-I", CSRC]
+          os.path.join(ROOT, "include"), "-I", CSRC,
+          "-I", os.path.join(CSRC, "paged")]
 NOISE = "is not a recognized feature for this target"
 
 

@@ -1,0 +1,729 @@
+// Attention over the paged cache (include/plora_paged.h, plora_attn_paged): the
+// items of the step's plan, then the merge of the partials.
+//
+// Both kernels compute transposed tiles: S^T = K Q^T, so that a lane holds scores
+// of one query row (its column) for several keys, then O^T = V^T P^T with P taken
+// straight from those registers: the matrix instruction's output layout gives a
+// lane groups of four keys, and since a product may sum its keys in any order, V
+// is brought into the same order.  No weight crosses a lane.  V^T needs, for one
+// dimension, eight keys in a lane: the lane loads eight rows and transposes the
+// 16-bit block in its own registers.
+// The scores are kept times scale log2(e), so a weight is one exp2 of one fma.
+
+#include <cmath>
+
+#include "attn_plan.h"
+
+namespace paged {
+namespace {
+
+constexpr int kNT = 256;
+constexpr int kWaves = kNT / 64;
+constexpr int kRsrcWord3 = 0x00020000;    // raw buffer, 32-bit data format (gfx9 family)
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+struct AttnArgs {
+  const uint16_t *q, *k, *v;
+  int64_t q_token, q_head, out_token, out_head, page_stride, head_stride;
+  int32_t key_stride, n_pages, log_page, max_pages;
+  const int32_t *table, *pos, *order, *req, *q_start;
+  const PlanHeader* head;
+  const Item *few, *tile;
+  const ReqInfo* info;
+  int32_t batch, T, r, kv_heads;
+  float c;                  // |scale| log2(e)
+  uint32_t flip;            // sign bits for q where scale < 0
+  uint16_t* out;
+  float *pm, *pl, *po;      // partials: [row][kv_heads], [row][kv_heads][D]
+};
+
+__device__ __forceinline__ f32x4 mfma16(Bf16, u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(Fp16, u32x4 a, u32x4 b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a),
+                                                __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32(Bf16, u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a),
+                                                 __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32(Fp16, u32x4 a, u32x4 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a),
+                                                __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+
+// Valid rows of 16 keys of one page and head as a raw buffer resource: what lies
+// past them, or in a page outside the pool, reads zero and fetches nothing.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t keys_rsrc(const AttnArgs& a, const uint16_t* x,
+                                                            const int32_t* row, int kvh, int key,
+                                                            int rows, int D) {
+  int page = -1;
+  if (rows > 0) page = row[key >> a.log_page];
+  page = uniform(page);
+  const bool ok = page >= 0 && page < a.n_pages;
+  const int64_t at = ok ? page * a.page_stride + kvh * a.head_stride +
+                              (int64_t)(key & ((1 << a.log_page) - 1)) * a.key_stride
+                        : 0;
+  const int bytes = ok ? ((min(rows, 16) - 1) * a.key_stride + D) * 2 : 0;
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(x) + at, 0, bytes, kRsrcWord3);
+}
+
+__device__ __forceinline__ u32x4 bld16(__amdgpu_buffer_rsrc_t r, int off) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+}
+__device__ __forceinline__ u32x2 bld8(__amdgpu_buffer_rsrc_t r, int off) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+}
+__device__ __forceinline__ uint32_t bld4(__amdgpu_buffer_rsrc_t r, int off) {
+  return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
+}
+
+// Words of 16-bit pairs (a's, b's) of the low or high halves.
+__device__ __forceinline__ uint32_t zip(uint32_t a, uint32_t b, bool high) {
+  return high ? __builtin_amdgcn_perm(b, a, 0x07060302u) : __builtin_amdgcn_perm(b, a, 0x05040100u);
+}
+
+// A query row: its token, its head, the keys it sees.
+struct Row {
+  int token, head, limit;
+};
+__device__ __forceinline__ Row query_row(const AttnArgs& a, const Item& it, int kvh, int i) {
+  Row x{0, 0, it.lo};
+  if (i < it.rows) {
+    const int R = it.row + i, tk = it.tok + R / a.r;
+    x.token = it.gathered ? a.order[tk] : tk;
+    x.head = kvh * a.r + R % a.r;
+    x.limit = max(it.lo, min(it.hi, a.pos[x.token] + 1));
+  }
+  return x;
+}
+
+// One row by itself, in vector arithmetic over the keys it sees and no others,
+// by one wavefront: 64 keys at a time, a lane a key for the scores and a lane D/64
+// dimensions for the output.  Taken where the tiles gave a row that is not finite:
+// they multiply the zero weight of a masked key with its value, which is not zero
+// if that value is an infinity or NaN.  Rare, and then the row's own infinities and
+// NaN come out as the sum gives them.
+template <class Ty, int D>
+__device__ __forceinline__ void careful_row(const AttnArgs& a, const Item& it, int kvh, int i) {
+  constexpr int kPer = D / 64;
+  const int lane = threadIdx.x & 63;
+  const Row x = query_row(a, it, kvh, i);
+  const uint16_t* q = a.q + x.token * a.q_token + x.head * a.q_head;
+  const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
+  float m = -INFINITY, l = 0.f, acc[kPer] = {};
+  for (int k0 = it.lo; k0 < x.limit; k0 += 64) {
+    const int n = min(64, x.limit - k0);
+    float s = -INFINITY;
+    if (lane < n) {
+      const int key = k0 + lane, page = row[key >> a.log_page];
+      s = 0.f;
+      if (page >= 0 && page < a.n_pages) {
+        const uint16_t* kp = a.k + page * a.page_stride + kvh * a.head_stride +
+                             (int64_t)(key & ((1 << a.log_page) - 1)) * a.key_stride;
+        for (int d = 0; d < D; d += 2) {
+          const uint32_t kw = *reinterpret_cast<const uint32_t*>(kp + d);
+          const uint32_t qw = *reinterpret_cast<const uint32_t*>(q + d) ^ a.flip;
+          s = fmaf(Ty::lo(kw), Ty::lo(qw), s);
+          s = fmaf(Ty::hi(kw), Ty::hi(qw), s);
+        }
+      }
+      s *= a.c;
+    }
+    float mx = s;
+    for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
+    mx = fmaxf(mx, m);
+    const float ms = mx == -INFINITY ? 0.f : mx;
+    const float al = exp2_(m - ms), p = exp2_(s - ms);
+    m = mx;
+    float t = p;
+    for (int d = 32; d; d >>= 1) t += __shfl_xor(t, d, 64);
+    l = l * al + t;
+    for (int j = 0; j < kPer; ++j) acc[j] *= al;
+    for (int j = 0; j < n; ++j) {
+      const int key = k0 + j, page = uniform(row[key >> a.log_page]);
+      const float w = __shfl(p, j, 64);
+      if (page < 0 || page >= a.n_pages) continue;
+      const uint16_t* vp = a.v + page * a.page_stride + kvh * a.head_stride +
+                           (int64_t)(key & ((1 << a.log_page) - 1)) * a.key_stride + kPer * lane;
+      for (int e = 0; e < kPer; ++e) acc[e] = fmaf(w, Ty::lo(vp[e]), acc[e]);
+    }
+  }
+  if (m == -INFINITY && x.limit > it.lo) l = NAN;     // every score -inf: 0 / 0
+  if (it.part < 0) {
+    uint16_t* o = a.out + x.token * a.out_token + x.head * a.out_head + kPer * lane;
+    for (int e = 0; e < kPer; ++e)
+      o[e] = (uint16_t)Ty::pack(x.limit > it.lo ? acc[e] / l : 0.f, 0.f);
+  } else {
+    const int64_t at = ((int64_t)it.part + i) * a.kv_heads + kvh;
+    if (lane == 0) a.pm[at] = m, a.pl[at] = l;
+    for (int e = 0; e < kPer; ++e) a.po[at * D + kPer * lane + e] = acc[e];
+  }
+}
+
+// Items of up to 16 rows (decode: the rows are a key head's query heads times the
+// request's new tokens).  Bound by reading K and V once: 16 rows cost the matrix
+// units a twentieth of that time, so every row count up to 16 takes one tile.  The
+// four wavefronts take 32 keys each in turn, straight from memory into registers
+// (K as the 16x16x32 product's rows: key n of 16, 16-byte units; V as rows of eight
+// keys), and join through LDS at the end.  The weights enter the product with V as
+// two values, hi + lo, which costs nothing here and keeps them to 16 bits.
+template <class Ty, int D>
+__global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
+  constexpr int kQ = D / 32;             // 16-byte units of a row, per lane
+  constexpr int kV = D / 16;             // dimensions per lane
+  constexpr int kPad = D + 4;
+  __shared__ float s_o[kWaves][kFew][kPad];
+  __shared__ float s_m[kWaves][kFew], s_l[kWaves][kFew];
+  __shared__ int s_bad;
+  const int item = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
+  if (item >= a.head->few) return;
+  const Item it = a.few[item];
+  if (it.rows <= 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
+  const int n = lane & 15, g = lane >> 4;
+  const Row x = query_row(a, it, kvh, n);
+  u32x4 qf[kQ];
+#pragma unroll
+  for (int j = 0; j < kQ; ++j) qf[j] = u32x4{0, 0, 0, 0};
+  if (n < it.rows) {
+    const uint16_t* q = a.q + x.token * a.q_token + x.head * a.q_head + 8 * g;
+#pragma unroll
+    for (int j = 0; j < kQ; ++j) qf[j] = *reinterpret_cast<const u32x4*>(q + 32 * j) ^ a.flip;
+  }
+  int most = x.limit, least = n < it.rows ? x.limit : INT32_MAX;
+#pragma unroll
+  for (int d = 1; d < 16; d <<= 1) {
+    most = max(most, __shfl_xor(most, d, 64));
+    least = min(least, __shfl_xor(least, d, 64));
+  }
+  most = uniform(most);
+  least = uniform(least);
+  if (tid == 0) s_bad = 0;
+  const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
+
+  float m = -INFINITY, l = 0.f;
+  f32x4 acc[kV];
+#pragma unroll
+  for (int d = 0; d < kV; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int k0 = it.lo + 32 * wv; k0 < most; k0 += 32 * kWaves) {
+    u32x4 kf[2][kQ];
+    uint32_t vw[8][kV / 2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int key = k0 + 16 * b;
+      const auto rk = keys_rsrc(a, a.k, row, kvh, key, most - key, D);
+#pragma unroll
+      for (int j = 0; j < kQ; ++j)
+        kf[b][j] = bld16(rk, (n * a.key_stride + 32 * j + 8 * g) * 2);
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int key = k0 + 16 * b;
+      const auto rv = keys_rsrc(a, a.v, row, kvh, key, most - key, D);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int off = ((4 * g + i) * a.key_stride + kV * n) * 2;
+        if constexpr (kV == 8) {
+          const u32x4 w = bld16(rv, off);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vw[4 * b + i][e] = w[e];
+        } else {
+          const u32x2 w = bld8(rv, off);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) vw[4 * b + i][e] = w[e];
+        }
+      }
+    }
+    f32x4 s[2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < kQ; ++j) s[b] = mfma16(Ty{}, kf[b][j], qf[j], s[b]);
+    }
+    float t[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = s[i >> 2][i & 3] * a.c;
+    if (k0 + 32 > least) {               // some row does not see all 32
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        t[i] = k0 + 16 * (i >> 2) + 4 * g + (i & 3) < x.limit ? t[i] : -INFINITY;
+    }
+    float mx = m;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mx = fmaxf(mx, t[i]);
+    mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
+    mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+    const float ms = mx == -INFINITY ? 0.f : mx;
+    const float al = exp2_(m - ms);
+    m = mx;
+    l *= al;
+    u32x4 ph, pl;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p0 = exp2_(t[2 * i] - ms), p1 = exp2_(t[2 * i + 1] - ms);
+      l += p0 + p1;
+      ph[i] = Ty::pack(p0, p1);
+      pl[i] = Ty::pack(p0 - Ty::lo(ph[i]), p1 - Ty::hi(ph[i]));
+    }
+#pragma unroll
+    for (int d = 0; d < kV; ++d) {
+      u32x4 vt;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) vt[i] = zip(vw[2 * i][d / 2], vw[2 * i + 1][d / 2], d & 1);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[d][i] *= al;
+      acc[d] = mfma16(Ty{}, vt, ph, acc[d]);
+      acc[d] = mfma16(Ty{}, vt, pl, acc[d]);
+    }
+  }
+  l += __shfl_xor(l, 16, 64);
+  l += __shfl_xor(l, 32, 64);
+  if (g == 0) s_m[wv][n] = m, s_l[wv][n] = l;
+  // acc[d][i] is the output's dimension kV (4 g + i) + d of row n
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+#pragma unroll
+    for (int d = 0; d < kV; ++d) s_o[wv][n][kV * (4 * g + i) + d] = acc[d][i];
+  __syncthreads();
+  const int i = tid >> 4, e = (tid & 15) * kV;
+  if (i < it.rows) {
+    const Row y = query_row(a, it, kvh, i);
+    float M = s_m[0][i];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][i]);
+    const float Ms = M == -INFINITY ? 0.f : M;
+    float L = 0.f, o[kV] = {};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = exp2_(s_m[w][i] - Ms);
+      L = fmaf(f, s_l[w][i], L);
+#pragma unroll
+      for (int d = 0; d < kV; ++d) o[d] = fmaf(f, s_o[w][i][e + d], o[d]);
+    }
+    const bool any = y.limit > it.lo;
+    if (M == -INFINITY && any) L = NAN;
+    bool fine = true;
+#pragma unroll
+    for (int d = 0; d < kV; ++d) fine = fine && fabsf(o[d]) < INFINITY;
+    if (!fine) atomicOr(&s_bad, 1 << i);
+    if (it.part < 0) {
+      uint16_t* out = a.out + y.token * a.out_token + y.head * a.out_head + e;
+      const float inv = any ? 1.f / L : 0.f;
+      uint32_t w[kV / 2];
+#pragma unroll
+      for (int d = 0; d < kV / 2; ++d) w[d] = Ty::pack(o[2 * d] * inv, o[2 * d + 1] * inv);
+      if constexpr (kV == 8) *reinterpret_cast<u32x4*>(out) = u32x4{w[0], w[1], w[2], w[3]};
+      else *reinterpret_cast<u32x2*>(out) = u32x2{w[0], w[1]};
+    } else {
+      const int64_t at = ((int64_t)it.part + i) * a.kv_heads + kvh;
+      if (e == 0) a.pm[at] = M, a.pl[at] = L;
+#pragma unroll
+      for (int d = 0; d < kV; d += 4)
+        *reinterpret_cast<f32x4*>(a.po + at * D + e + d) = f32x4{o[d], o[d + 1], o[d + 2], o[d + 3]};
+    }
+  }
+  __syncthreads();
+  for (int b = wv; b < it.rows; b += kWaves)
+    if (s_bad >> b & 1) careful_row<Ty, D>(a, it, kvh, b);
+}
+
+// Items of up to 128 rows: prompts, and prefixes that many rows share.  A wavefront
+// has 32 rows; K and V go through LDS, 64 keys at a time, two buffers: the next
+// keys are loaded into registers while the present ones are used, and stored after.
+// K rows keep their order with 16-byte units turned by the row number (a read takes
+// one unit of 32 rows); V is transposed by its loader, so a lane reads the eight
+// keys of one dimension as one unit.  A row's maximum is only raised when a score
+// passes it by more than 8 (in powers of two), so the output is rarely rescaled:
+// weights are at most 2^8 then, of the same relative precision.
+// The weights enter the product with V rounded once to the type: this product
+// bounds the kernel, and their rounding errors average out below the output's own.
+// Bound by the matrix units and the exponentials together (for 64 keys and 32 rows
+// 1024 cycles of products, about as many of vector work).
+constexpr float kSlack = 8.f;
+
+template <class Ty, int D>
+__global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
+  constexpr int kQ = D / 16;                // products over a row
+  constexpr int kV = D / 32;                // dimensions per lane
+  constexpr int kU = D / 8;                 // 16-byte units of a row
+  constexpr int kRowsPer = kNT / kU;        // K rows loaded at a time
+  constexpr int kKL = kTileStep / kRowsPer; // K units per thread
+  __shared__ u32x4 s_k[2][kTileStep * kU];
+  __shared__ u32x4 s_v[2][8 * kV * 32];
+  __shared__ int s_most[kWaves];
+  const int item = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
+  if (item >= a.head->tiles) return;
+  const Item it = a.tile[item];
+  if (it.rows <= 0) return;
+  const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
+  const int n = lane & 31, h = lane >> 5;
+  const Row x = query_row(a, it, kvh, 32 * wv + n);
+  const bool mine = 32 * wv + n < it.rows;
+  u32x4 qf[kQ];
+#pragma unroll
+  for (int j = 0; j < kQ; ++j) qf[j] = u32x4{0, 0, 0, 0};
+  if (mine) {
+    const uint16_t* q = a.q + x.token * a.q_token + x.head * a.q_head + 8 * h;
+#pragma unroll
+    for (int j = 0; j < kQ; ++j) qf[j] = *reinterpret_cast<const u32x4*>(q + 16 * j) ^ a.flip;
+  }
+  int most = x.limit, least = mine ? x.limit : INT32_MAX;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    most = max(most, __shfl_xor(most, d, 64));
+    least = min(least, __shfl_xor(least, d, 64));
+  }
+  most = uniform(most);                     // of this wavefront
+  least = uniform(least);
+  if (lane == 0) s_most[wv] = most;
+  __syncthreads();
+  int end = s_most[0];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) end = max(end, s_most[w]);
+  end = uniform(end);
+  const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
+
+  // loaders: K rows kr + i kRowsPer, unit ku; V rows of octet o = tid / 32, kV
+  // dimensions from kV n.  The rows of one load lie in 16 keys of one page for
+  // each wavefront.
+  const int kr = tid / kU, ku = tid % kU;
+  const int kg = uniform(kr >> 4), ko = kr & 15;
+  const int oh = h;                         // octet 2 wv + h: keys 16 wv + 4 h + {0..3, 8..11}
+  u32x4 kreg[kKL];
+  uint32_t vreg[8][(kV + 1) / 2];
+  const auto fetch = [&](int k0) {
+#pragma unroll
+    for (int i = 0; i < kKL; ++i) {
+      const int key = k0 + 16 * (kg + i * (kRowsPer / 16));
+      const auto r = keys_rsrc(a, a.k, row, kvh, key, end - key, D);
+      kreg[i] = bld16(r, (ko * a.key_stride + 8 * ku) * 2);
+    }
+    const int key = k0 + 16 * wv;
+    const auto r = keys_rsrc(a, a.v, row, kvh, key, end - key, D);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int off = ((4 * oh + (i & 3) + 8 * (i >> 2)) * a.key_stride + kV * n) * 2;
+      if constexpr (kV == 4) {
+        const u32x2 w = bld8(r, off);
+        vreg[i][0] = w[0], vreg[i][1] = w[1];
+      } else {
+        vreg[i][0] = bld4(r, off);
+      }
+    }
+  };
+  const auto put = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < kKL; ++i) {
+      const int rw = kr + i * kRowsPer;
+      s_k[buf][rw * kU + (ku ^ (rw & (kU - 1)))] = kreg[i];
+    }
+#pragma unroll
+    for (int d = 0; d < kV; ++d) {
+      u32x4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = zip(vreg[2 * i][d / 2], vreg[2 * i + 1][d / 2], d & 1);
+      s_v[buf][((2 * wv + h) * kV + d) * 32 + n] = w;
+    }
+  };
+
+  float m = -INFINITY, l = 0.f;
+  f32x16 acc[kV];
+#pragma unroll
+  for (int d = 0; d < kV; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+  if (it.lo < end) {
+    fetch(it.lo);
+    put(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int k0 = it.lo; k0 < end; k0 += kTileStep, buf ^= 1) {
+    const bool more = k0 + kTileStep < end;
+    if (more) fetch(k0 + kTileStep);
+    if (k0 < most) {
+      f32x16 s[2];
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
+        const int rw = 32 * b + n;
+#pragma unroll
+        for (int j = 0; j < kQ; ++j)
+          s[b] = mfma32(Ty{}, s_k[buf][rw * kU + ((2 * j + h) ^ (rw & (kU - 1)))], qf[j], s[b]);
+      }
+      // s[b][i] is key 32 b + 8 (i / 4) + 4 h + i % 4 of row n
+      if (k0 + kTileStep > least) {
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            s[b][i] = k0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) < x.limit ? s[b][i] : -INFINITY;
+      }
+      float mx = -INFINITY;
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+      mx *= a.c;
+      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+      if (__any(mx > m + kSlack)) {
+        const float mn = fmaxf(m, mx), ms = mn == -INFINITY ? 0.f : mn;
+        const float al = exp2_(m - ms);
+        m = mn;
+        l *= al;
+#pragma unroll
+        for (int d = 0; d < kV; ++d)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[d][i] *= al;
+      }
+      const float ms = m == -INFINITY ? 0.f : m;
+      u32x4 p[4];
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float p0 = exp2_(fmaf(s[b][2 * i], a.c, -ms));
+          const float p1 = exp2_(fmaf(s[b][2 * i + 1], a.c, -ms));
+          l += p0 + p1;
+          p[2 * b + (i >> 2)][i & 3] = Ty::pack(p0, p1);
+        }
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int d = 0; d < kV; ++d)
+          acc[d] = mfma32(Ty{}, s_v[buf][((2 * b + h) * kV + d) * 32 + n], p[b], acc[d]);
+    }
+    if (more) put(buf ^ 1);
+    __syncthreads();
+  }
+  if (32 * wv >= it.rows) return;
+  l += __shfl_xor(l, 32, 64);
+  const bool any = x.limit > it.lo;
+  if (m == -INFINITY && any) l = NAN;
+  // acc[d][i] is the output's dimension kV (8 (i / 4) + 4 h + i % 4) + d of row n
+  bool fine = true;
+#pragma unroll
+  for (int d = 0; d < kV; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) fine = fine && fabsf(acc[d][i]) < INFINITY;
+  if (mine) {
+    if (it.part < 0) {
+      uint16_t* out = a.out + x.token * a.out_token + x.head * a.out_head;
+      const float inv = any ? 1.f / l : 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        uint16_t* o = out + kV * (8 * (i >> 2) + 4 * h + (i & 3));
+        const uint32_t w0 = Ty::pack(acc[0][i] * inv, acc[1][i] * inv);
+        if constexpr (kV == 4)
+          *reinterpret_cast<u32x2*>(o) = u32x2{w0, Ty::pack(acc[2][i] * inv, acc[3][i] * inv)};
+        else
+          *reinterpret_cast<uint32_t*>(o) = w0;
+      }
+    } else {
+      const int64_t at = ((int64_t)it.part + 32 * wv + n) * a.kv_heads + kvh;
+      if (h == 0) a.pm[at] = m, a.pl[at] = l;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float* o = a.po + at * D + kV * (8 * (i >> 2) + 4 * h + (i & 3));
+#pragma unroll
+        for (int d = 0; d < kV; ++d) o[d] = acc[d][i];
+      }
+    }
+  }
+  uint64_t bad = __ballot(mine && !fine);
+  bad = (bad | bad >> 32) & 0xffffffffu;
+  while (bad) {
+    const int i = __builtin_ctzll(bad);
+    bad &= bad - 1;
+    careful_row<Ty, D>(a, it, kvh, 32 * wv + i);
+  }
+}
+
+// Joins a row's partials: its request's own pieces, then its prefix's.  One
+// wavefront a row; the weights of up to 64 pieces are found at once, a lane a
+// piece.  Rows that the items wrote themselves are left, rows without a key
+// get zeros.  Bound by reading the partials, or by latency.
+template <class Ty, int D>
+__global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
+  constexpr int kPer = D / 64;
+  const int t = blockIdx.x, lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+  const int b = a.req[t], heads = a.kv_heads * a.r;
+  ReqInfo f{};
+  int R0 = 0;
+  if (b >= 0 && b < a.batch && t >= a.q_start[b] && t < a.q_start[b + 1]) {
+    f = a.info[b];
+    R0 = (t - a.q_start[b]) * a.r;
+  }
+  if (f.state == 2) return;
+  const int end = min(heads, ((int)blockIdx.y + 1) * per);
+  for (int hd = blockIdx.y * per + wv; hd < end; hd += kWaves) {
+    const int kvh = hd / a.r, R = R0 + hd % a.r;
+    uint16_t* out = a.out + t * a.out_token + hd * a.out_head + kPer * lane;
+    const int own = f.state == 1 ? f.splits : 0, pre = f.state == 1 && f.pre_part >= 0 ? f.pre_splits : 0;
+    const int pieces = own + pre;
+    float M = -INFINITY, L = 0.f, o[kPer] = {};
+    for (int p0 = 0; p0 < pieces; p0 += 64) {
+      const int p = p0 + lane, n = min(64, pieces - p0);
+      int64_t at = 0;
+      float m = -INFINITY, l = 0.f;
+      if (p < pieces) {
+        at = p < own ? (int64_t)f.part + (int64_t)p * f.rows + R
+                     : (int64_t)f.pre_part + (int64_t)(p - own) * f.pre_rows + f.pre_row + R;
+        at = at * a.kv_heads + kvh;
+        m = a.pm[at], l = a.pl[at];
+      }
+      float mx = m;
+      for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
+      mx = fmaxf(mx, M);
+      const float ms = mx == -INFINITY ? 0.f : mx, al = exp2_(M - ms);
+      if (M == -INFINITY && mx > -INFINITY) L = 0.f;
+      M = mx;
+      // a piece whose scores are all -inf (its l is NaN) weighs nothing beside
+      // others; alone it makes the row NaN
+      const float w = exp2_(m - ms);
+      float s = m > -INFINITY ? w * l : mx > -INFINITY ? 0.f : l;
+      for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d, 64);
+      L = (M > -INFINITY ? L * al : L) + s;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) o[e] *= al;
+      for (int j = 0; j < n; ++j) {
+        const float wj = __shfl(w, j, 64);
+        const int64_t aj = __shfl(at, j, 64);
+        const float* po = a.po + aj * D + kPer * lane;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] = fmaf(wj, po[e], o[e]);
+      }
+    }
+    const bool none = M == -INFINITY && L == 0.f;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) o[e] = none ? 0.f : o[e] / L;
+    if constexpr (kPer == 2) *reinterpret_cast<uint32_t*>(out) = Ty::pack(o[0], o[1]);
+    else *out = (uint16_t)Ty::pack(o[0], 0.f);
+  }
+}
+
+struct WsLayout {
+  size_t l, o, bytes;
+};
+WsLayout ws_layout(const plora_attn_shape& s, const Bounds& b) {
+  WsLayout w{};
+  const size_t n = (size_t)b.part_rows * s.kv_heads;
+  w.l = align256(n * 4);
+  w.o = w.l + align256(n * 4);
+  w.bytes = w.o + align256(n * s.head_dim * 4);
+  return w;
+}
+
+template <class Ty, int D>
+plora_status launch(const AttnArgs& a, const Bounds& b, hipStream_t stream) {
+  clear_error();
+  hipLaunchKernelGGL((few_kernel<Ty, D>), dim3(b.few_cap * a.kv_heads), dim3(kNT), 0, stream, a);
+  plora_status st = launch_status();
+  if (st != PLORA_OK) return st;
+  if (b.tile_cap > 0) {
+    hipLaunchKernelGGL((tile_kernel<Ty, D>), dim3(b.tile_cap * a.kv_heads), dim3(kNT), 0, stream,
+                       a);
+    st = launch_status();
+    if (st != PLORA_OK) return st;
+  }
+  // heads of a token per work group: all, or four where the tokens are few
+  const int heads = a.kv_heads * a.r, per = a.T < 512 ? kWaves : heads;
+  hipLaunchKernelGGL((merge_kernel<Ty, D>), dim3(a.T, (heads + per - 1) / per), dim3(kNT), 0,
+                     stream, a, per);
+  return launch_status();
+}
+
+}  // namespace
+}  // namespace paged
+
+extern "C" size_t plora_attn_paged_workspace_bytes(const plora_attn_shape* shape) {
+  using namespace paged;
+  if (!shape || !shape_ok(*shape) || shape_empty(*shape)) return 0;
+  return ws_layout(*shape, bounds(*shape)).bytes;
+}
+
+extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t q_head,
+                                         const plora_kv_cache* cache, const plora_kv_step* step,
+                                         const plora_attn_shape* shape, float scale,
+                                         const void* plan, size_t plan_bytes, void* out,
+                                         int64_t out_token, int64_t out_head, void* ws,
+                                         size_t ws_bytes, hipStream_t stream) {
+  using namespace paged;
+  if (!cache || !step || !shape) return PLORA_ERR_INVALID_ARG;
+  const plora_attn_shape& s = *shape;
+  const plora_kv_cache& c = *cache;
+  if (s.batch < 0 || s.T < 0 || s.heads < 0 || s.kv_heads < 0 || s.max_q < 0 ||
+      step->batch != s.batch || step->T != s.T || c.kv_heads != s.kv_heads ||
+      c.head_dim != s.head_dim || c.page_size != step->page_size || c.n_pages < 0 ||
+      step->max_pages < 0 || q_token < 0 || q_head < 0 || out_token < 0 || out_head < 0 ||
+      c.page_stride < 0 || c.head_stride < 0 || c.token_stride < 0 || !std::isfinite(scale))
+    return PLORA_ERR_INVALID_ARG;
+  if (!shape_ok(s) || !page_size_ok(c.page_size) ||
+      (c.dtype != PLORA_BF16 && c.dtype != PLORA_FP16))
+    return PLORA_ERR_UNSUPPORTED;
+  if (shape_empty(s)) return PLORA_OK;
+  if (c.token_stride < s.head_dim) return PLORA_ERR_INVALID_ARG;
+  if (q_token % 8 || q_head % 8 || out_token % 8 || out_head % 8 || c.page_stride % 8 ||
+      c.head_stride % 8 || c.token_stride % 8 || c.token_stride > (INT32_MAX / 4) / 16)
+    return PLORA_ERR_UNSUPPORTED;
+  if (!q || !out || !plan || !ws || !step->pos || !step->req || !step->q_start ||
+      (c.n_pages > 0 && (!c.k || !c.v)) || (step->max_pages > 0 && !step->table))
+    return PLORA_ERR_INVALID_ARG;
+  if (!aligned(q, 16) || !aligned(out, 16) || !aligned(plan, 16) || !aligned(ws, 16) ||
+      !aligned(c.k, 16) || !aligned(c.v, 16))
+    return PLORA_ERR_UNSUPPORTED;
+  const Bounds b = bounds(s);
+  const PlanLayout l = plan_layout(s, b);
+  const WsLayout w = ws_layout(s, b);
+  if (plan_bytes < l.bytes || ws_bytes < w.bytes) return PLORA_ERR_WORKSPACE_TOO_SMALL;
+  if ((int64_t)std::max(b.few_cap, b.tile_cap) * s.kv_heads > INT32_MAX)
+    return PLORA_ERR_UNSUPPORTED;
+  const char* p = static_cast<const char*>(plan);
+  AttnArgs a{};
+  a.q = static_cast<const uint16_t*>(q);
+  a.k = static_cast<const uint16_t*>(c.k);
+  a.v = static_cast<const uint16_t*>(c.v);
+  a.q_token = q_token;
+  a.q_head = q_head;
+  a.out_token = out_token;
+  a.out_head = out_head;
+  a.page_stride = c.page_stride;
+  a.head_stride = c.head_stride;
+  a.key_stride = (int32_t)c.token_stride;
+  a.n_pages = c.n_pages;
+  a.log_page = log2_of(c.page_size);
+  a.max_pages = step->max_pages;
+  a.table = step->table;
+  a.pos = step->pos;
+  a.req = step->req;
+  a.q_start = step->q_start;
+  a.head = reinterpret_cast<const PlanHeader*>(p);
+  a.few = reinterpret_cast<const Item*>(p + l.few);
+  a.tile = reinterpret_cast<const Item*>(p + l.tile);
+  a.order = reinterpret_cast<const int32_t*>(p + l.order);
+  a.info = reinterpret_cast<const ReqInfo*>(p + l.req);
+  a.batch = s.batch;
+  a.T = s.T;
+  a.r = b.r;
+  a.kv_heads = s.kv_heads;
+  // (a scale of 0 keeps masked scores at -inf with the smallest factor instead)
+  a.c = std::max(std::fabs(scale) * 1.44269504f, 1.17549435e-38f);
+  a.flip = scale < 0.f ? 0x80008000u : 0u;
+  a.out = static_cast<uint16_t*>(out);
+  char* wp = static_cast<char*>(ws);
+  a.pm = reinterpret_cast<float*>(wp);
+  a.pl = reinterpret_cast<float*>(wp + w.l);
+  a.po = reinterpret_cast<float*>(wp + w.o);
+  if (c.dtype == PLORA_BF16)
+    return s.head_dim == 128 ? launch<Bf16, 128>(a, b, stream) : launch<Bf16, 64>(a, b, stream);
+  return s.head_dim == 128 ? launch<Fp16, 128>(a, b, stream) : launch<Fp16, 64>(a, b, stream);
+}

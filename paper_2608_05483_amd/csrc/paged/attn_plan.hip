@@ -1,0 +1,353 @@
+// The work of a step's attention, built on the GPU (include/plora_paged.h,
+// plora_attn_plan): which query rows read which keys, in items of about equal work.
+
+#include "attn_plan.h"
+
+namespace paged {
+namespace {
+
+constexpr int kNT = 512;
+constexpr int kWaves = kNT / 64;
+
+struct PlanArgs {
+  int32_t batch, T, r, kv_heads, max_q, page_size;
+  int64_t max_keys;
+  const int32_t *q_start, *kv_len, *req;
+  // groups
+  int32_t shared, n_groups, cap;
+  const int32_t *perm, *seg_ptr, *seg_id, *meta, *prefix_len;
+  // plan
+  PlanHeader* head;
+  Item *few, *tile;
+  int32_t* order;
+  ReqInfo* info;
+  int32_t *u_len, *place, *seg_of, *moff, *seg_part;   // [batch + 1] each, groups only
+  int32_t few_cap, tile_cap;
+  int64_t part_cap;
+};
+
+// Exclusive scan of one value a thread over the work group; total is the sum.
+__device__ __forceinline__ int64_t scan(int64_t x, int64_t* red, int64_t& total) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  int64_t inc = x;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const int64_t y = __shfl_up(inc, d, 64);
+    if (lane >= d) inc += y;
+  }
+  if (lane == 63) red[wv] = inc;
+  __syncthreads();
+  int64_t before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wv) before += red[w];
+    all += red[w];
+  }
+  __syncthreads();
+  total = all;
+  return before + inc - x;
+}
+
+// A request's new tokens, 0 if it has none or the step left it out.
+__device__ __forceinline__ int tokens(const PlanArgs& a, int b, int& q0, int& kv) {
+  q0 = a.q_start[b];
+  kv = a.kv_len[b];
+  const int q1 = a.q_start[b + 1];
+  if (q0 < 0 || q0 >= q1 || q1 > a.T || a.req[q0] != b) return 0;
+  const int n = q1 - q0;
+  return n > a.max_q || kv < n || kv > a.max_keys ? 0 : n;
+}
+
+// The whole pages of a group's prefix, in keys.
+__device__ __forceinline__ int prefix(const PlanArgs& a, int seg) {
+  const int g = a.seg_id[seg];
+  if (g < 0 || g >= a.n_groups) return 0;
+  const int64_t u = min((int64_t)a.prefix_len[g], a.max_keys);
+  return u <= 0 ? 0 : (int)(u & -(int64_t)a.page_size);
+}
+
+// How a set of rows x keys is cut.
+struct Cut {
+  int tiles, pieces, keys;   // keys per piece
+  bool few;
+};
+__device__ __forceinline__ Cut cut(int rows, int keys, int few_keys, int tile_keys) {
+  Cut c;
+  c.few = rows <= kFew;
+  c.tiles = c.few ? 1 : (rows + kTile - 1) / kTile;
+  const int most = c.few ? few_keys : tile_keys, step = c.few ? kFewStep : kTileStep;
+  const int n = (keys - 1) / most + 1;                   // keys >= 1
+  c.keys = ((keys - 1) / n + 1 + step - 1) / step * step;
+  c.pieces = (keys - 1) / c.keys + 1;                    // <= n
+  return c;
+}
+
+// First place of a segment in perm.
+__device__ __forceinline__ int seg_begin(const PlanArgs& a, int s, int n_valid) {
+  return min(max(a.seg_ptr[s], 0), n_valid);
+}
+
+struct Set {
+  int32_t tok, rows, req, lo, hi, part, gathered;
+  Cut c;
+  int64_t base;              // first item
+};
+
+// One work group.  Three passes over the requests: the members of the groups and
+// their tokens in group order; the work of each kind, which sets the keys per piece;
+// the items (scans give each set its place, then a wavefront a set writes them).
+// Integer sums only, in a fixed order (the counts of members are sums by atomics,
+// whose order does not matter).
+// Pieces: C = work / (target / kv_heads) keys, at least kMinFew / kMinTile, so that
+// about target work groups of equal work come out; sets of fewer keys stay whole.
+// Once a step and bound by latency: its dependent loads and its scans.
+constexpr int kMinFew = 256, kMinTile = 256;
+
+__global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
+  __shared__ int64_t red[kWaves];
+  __shared__ Set sets[kNT];
+  __shared__ int s_few_keys, s_tile_keys;
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  int n_seg = 0, n_valid = 0;
+  int64_t total;
+  if (a.shared) {
+    n_seg = min(max(a.meta[0], 0), a.cap);
+    n_valid = min(max(a.meta[1], 0), a.batch);
+    for (int i = tid; i <= a.batch; i += kNT) a.u_len[i] = 0, a.seg_part[i] = 0;
+    __syncthreads();
+    // who could share
+    for (int p = tid; p < n_valid; p += kNT) {
+      const int b = a.perm[p];
+      if (b < 0 || b >= a.batch) continue;
+      int s = 0, z = n_seg;                              // the segment that holds p
+      while (z - s > 1) {
+        const int mid = (s + z) >> 1;
+        if (a.seg_ptr[mid] <= p) s = mid;
+        else z = mid;
+      }
+      int q0, kv;
+      const int n = tokens(a, b, q0, kv), u = n_seg > 0 ? prefix(a, s) : 0;
+      a.seg_of[b] = s;
+      if (n > 0 && u > 0 && (int64_t)n * a.r <= PLORA_ATTN_SHARE_ROWS && kv - n >= u) {
+        a.u_len[b] = u;
+        atomicAdd(&a.seg_part[s], 1);
+      }
+    }
+    __syncthreads();
+    // members: not alone in their group; their tokens in group order
+    int64_t carry = 0;
+    for (int p0 = 0; p0 < n_valid; p0 += kNT) {
+      const int p = p0 + tid;
+      int b = p < n_valid ? a.perm[p] : -1, q0 = 0, kv, n = 0;
+      if (b < 0 || b >= a.batch) b = -1;
+      if (b >= 0 && a.u_len[b] > 0) {
+        if (a.seg_part[a.seg_of[b]] >= 2) n = tokens(a, b, q0, kv);
+        else a.u_len[b] = 0;
+      }
+      const int64_t at = carry + scan(n, red, total);
+      carry += total;
+      if (p < n_valid) a.moff[p] = (int)at;
+      if (n > 0) {
+        a.place[b] = (int)at;
+        for (int j = 0; j < n; ++j)
+          if (at + j < a.T) a.order[at + j] = q0 + j;
+      }
+    }
+    if (tid == 0) a.moff[n_valid] = (int)carry;
+    __syncthreads();
+  }
+  // work of each kind: tiles x keys
+  int64_t few_work = 0, tile_work = 0;
+  const auto add = [&](int64_t rows, int keys) {
+    if (rows <= 0 || keys <= 0) return;
+    if (rows <= kFew) few_work += keys;
+    else tile_work += (rows + kTile - 1) / kTile * keys;
+  };
+  for (int s = tid; s < n_seg; s += kNT)
+    add((int64_t)(a.moff[seg_begin(a, s + 1, n_valid)] - a.moff[seg_begin(a, s, n_valid)]) * a.r,
+        prefix(a, s));
+  for (int b = tid; b < a.batch; b += kNT) {
+    int q0, kv;
+    const int n = tokens(a, b, q0, kv);
+    add((int64_t)n * a.r, kv - (a.shared ? a.u_len[b] : 0));
+  }
+  const auto pieces = [&](int64_t work, int target, int least, int step) {
+    const int64_t t = (target + a.kv_heads - 1) / a.kv_heads;
+    const int64_t c = max((work + t - 1) / t, (int64_t)least);
+    return (int)min((c + step - 1) / step * step, (int64_t)PLORA_PAGED_MAX_KEYS);
+  };
+  scan(few_work, red, total);
+  if (tid == 0) s_few_keys = pieces(total, kFewTarget, kMinFew, kFewStep);
+  scan(tile_work, red, total);
+  if (tid == 0) s_tile_keys = pieces(total, kTileTarget, kMinTile, kTileStep);
+  __syncthreads();
+  const int few_keys = s_few_keys, tile_keys = s_tile_keys;
+  // items: the groups' prefixes first, then the requests' own keys
+  int64_t few_n = 0, tile_n = 0, part_n = 0;
+  for (int pass = a.shared ? 0 : 1; pass < 2; ++pass) {
+    const int count = pass == 0 ? n_seg : a.batch;
+    for (int i0 = 0; i0 < count; i0 += kNT) {
+      const int i = i0 + tid, m = min(kNT, count - i0);
+      Set x{};
+      x.req = -1;
+      int64_t rows = 0;
+      int u = 0;
+      if (i < count && pass == 0) {
+        const int p0 = seg_begin(a, i, n_valid), p1 = seg_begin(a, i + 1, n_valid);
+        x.tok = a.moff[p0];
+        rows = (int64_t)(a.moff[p1] - x.tok) * a.r;
+        x.hi = prefix(a, i);
+        x.gathered = 1;
+        if (rows > 0) x.req = a.req[a.order[min(x.tok, a.T - 1)]];
+      } else if (i < count) {
+        int q0, kv;
+        const int n = tokens(a, i, q0, kv);
+        u = a.shared ? a.u_len[i] : 0;
+        rows = (int64_t)n * a.r;
+        x.tok = q0;
+        x.req = i;
+        x.lo = u;
+        x.hi = kv;
+      }
+      if (rows <= 0 || rows > INT32_MAX || x.hi <= x.lo) rows = 0;
+      x.rows = (int)rows;
+      int64_t items = 0, part = 0;
+      if (rows > 0) {
+        x.c = cut(x.rows, x.hi - x.lo, few_keys, tile_keys);
+        items = (int64_t)x.c.tiles * x.c.pieces;
+        part = pass == 0 || u > 0 || x.c.pieces > 1 ? rows * x.c.pieces : 0;
+      }
+      int64_t few_total, tile_total, part_total;
+      const int64_t fb = few_n + scan(x.c.few ? items : 0, red, few_total);
+      const int64_t tb = tile_n + scan(x.c.few ? 0 : items, red, tile_total);
+      const int64_t pb = part_n + scan(part, red, part_total);
+      // (never past the caps for lengths that agree with the shape)
+      const bool fits = (x.c.few ? fb + items <= a.few_cap : tb + items <= a.tile_cap) &&
+                        pb + part <= a.part_cap;
+      if (!fits) x.rows = 0;
+      x.base = x.c.few ? fb : tb;
+      x.part = part > 0 ? (int)pb : -1;
+      if (i < count && pass == 0) a.seg_part[i] = x.rows > 0 ? x.part : -1;
+      if (i < count && pass == 1) {
+        ReqInfo f{};
+        f.part = x.part;
+        f.splits = x.c.pieces;
+        f.rows = x.rows;
+        f.pre_part = -1;
+        f.state = x.rows == 0 ? 0 : x.part < 0 ? 2 : 1;
+        if (u > 0 && x.rows > 0) {
+          const int s = a.seg_of[i], t0 = a.moff[seg_begin(a, s, n_valid)];
+          const int all = (a.moff[seg_begin(a, s + 1, n_valid)] - t0) * a.r;
+          f.pre_part = a.seg_part[s];
+          f.pre_rows = all;
+          f.pre_splits = cut(all, u, few_keys, tile_keys).pieces;
+          f.pre_row = (a.place[i] - t0) * a.r;
+          if (f.pre_part < 0) f.state = 0;
+        }
+        a.info[i] = f;
+      }
+      sets[tid] = x;
+      __syncthreads();
+      for (int k = wv; k < m; k += kWaves) {
+        const Set& y = sets[k];
+        Item* list = y.c.few ? a.few : a.tile;
+        const int64_t cap = y.c.few ? a.few_cap : a.tile_cap;
+        const int64_t items = min((int64_t)y.c.tiles * y.c.pieces, cap - y.base);
+        for (int j = lane; j < items; j += 64) {
+          // the last rows, which see the most keys, first
+          const int tile = y.c.tiles - 1 - j / y.c.pieces, piece = j % y.c.pieces;
+          Item it;
+          it.tok = y.tok;
+          it.row = tile * kTile;
+          it.rows = min(y.rows - it.row, kTile);      // none if the set did not fit
+          it.req = y.req;
+          it.lo = y.lo + piece * y.c.keys;
+          it.hi = min(y.hi, it.lo + y.c.keys);
+          it.part = y.part < 0 ? -1 : y.part + piece * y.rows + it.row;
+          it.gathered = y.gathered;
+          list[y.base + j] = it;
+        }
+      }
+      __syncthreads();
+      few_n += few_total;
+      tile_n += tile_total;
+      part_n += part_total;
+    }
+  }
+  if (tid == 0)
+    *a.head = {(int)min(few_n, (int64_t)a.few_cap), (int)min(tile_n, (int64_t)a.tile_cap),
+               (int)min(part_n, a.part_cap), few_keys, tile_keys};
+}
+
+}  // namespace
+}  // namespace paged
+
+extern "C" size_t plora_attn_plan_bytes(const plora_attn_shape* shape) {
+  using namespace paged;
+  if (!shape || !shape_ok(*shape) || shape_empty(*shape)) return 0;
+  return plan_layout(*shape, bounds(*shape)).bytes;
+}
+
+extern "C" plora_status plora_attn_plan(const plora_kv_step* step, const plora_attn_shape* shape,
+                                        const plora_segments* seg, const int32_t* prefix_len,
+                                        int32_t n_groups, void* plan, size_t plan_bytes,
+                                        hipStream_t stream) {
+  using namespace paged;
+  if (!step || !shape || step->batch != shape->batch || step->T != shape->T || n_groups < 0 ||
+      step->max_pages < 0 || (seg && !shape->shared) || (seg && seg->T != shape->batch))
+    return PLORA_ERR_INVALID_ARG;
+  if (shape->batch < 0 || shape->T < 0 || shape->heads < 0 || shape->kv_heads < 0 ||
+      shape->max_q < 0)
+    return PLORA_ERR_INVALID_ARG;
+  if (!shape_ok(*shape) || !page_size_ok(step->page_size)) return PLORA_ERR_UNSUPPORTED;
+  if (shape_empty(*shape)) return PLORA_OK;
+  if (!step->q_start || !step->kv_len || !step->req || !plan) return PLORA_ERR_INVALID_ARG;
+  if (seg && (!prefix_len || !seg->perm || !seg->seg_ptr || !seg->seg_id || !seg->meta ||
+              seg->cap != std::min(seg->T, n_groups)))
+    return PLORA_ERR_INVALID_ARG;
+  if (!aligned(plan, 16)) return PLORA_ERR_UNSUPPORTED;
+  const Bounds b = bounds(*shape);
+  const PlanLayout l = plan_layout(*shape, b);
+  if (plan_bytes < l.bytes) return PLORA_ERR_WORKSPACE_TOO_SMALL;
+  char* base = static_cast<char*>(plan);
+  PlanArgs a{};
+  a.batch = shape->batch;
+  a.T = shape->T;
+  a.r = b.r;
+  a.kv_heads = shape->kv_heads;
+  a.max_q = shape->max_q;
+  a.page_size = step->page_size;
+  a.max_keys = std::min((int64_t)step->max_pages * step->page_size,
+                        (int64_t)PLORA_PAGED_MAX_KEYS);
+  a.q_start = step->q_start;
+  a.kv_len = step->kv_len;
+  a.req = step->req;
+  a.head = reinterpret_cast<PlanHeader*>(base);
+  a.few = reinterpret_cast<Item*>(base + l.few);
+  a.tile = reinterpret_cast<Item*>(base + l.tile);
+  a.order = reinterpret_cast<int32_t*>(base + l.order);
+  a.info = reinterpret_cast<ReqInfo*>(base + l.req);
+  a.few_cap = b.few_cap;
+  a.tile_cap = b.tile_cap;
+  a.part_cap = b.part_rows;
+  if (seg && n_groups > 0) {
+    a.shared = 1;
+    a.n_groups = n_groups;
+    a.cap = seg->cap;
+    a.perm = seg->perm;
+    a.seg_ptr = seg->seg_ptr;
+    a.seg_id = seg->seg_id;
+    a.meta = seg->meta;
+    a.prefix_len = prefix_len;
+    int32_t* s = reinterpret_cast<int32_t*>(base + l.scratch);
+    const int32_t n = shape->batch + 1;
+    a.u_len = s;
+    a.place = s + n;
+    a.seg_of = s + 2 * n;
+    a.moff = s + 3 * n;
+    a.seg_part = s + 4 * n;
+  }
+  clear_error();
+  hipLaunchKernelGGL(attn_plan_kernel, dim3(1), dim3(kNT), 0, stream, a);
+  return launch_status();
+}

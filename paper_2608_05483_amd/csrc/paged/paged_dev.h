@@ -1,0 +1,71 @@
+// Shared by the kernels of include/plora_paged.h: 16-bit types, checks, status.
+#ifndef PLORA_PAGED_DEV_H
+#define PLORA_PAGED_DEV_H
+
+#include <hip/hip_runtime.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "plora_paged.h"
+
+namespace paged {
+
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// The two 16-bit types: unpacking, rounding to nearest even, and the bits
+// that only infinities and NaN have all set.
+struct Bf16 {
+  static constexpr uint32_t kExp = 0x7f80u;
+  __device__ static __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
+  __device__ static __forceinline__ float hi(uint32_t w) {
+    return __uint_as_float(w & 0xffff0000u);
+  }
+  __device__ static __forceinline__ uint32_t pack(float a, float b) {
+    const bf16x2 v = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, v);
+  }
+};
+struct Fp16 {
+  static constexpr uint32_t kExp = 0x7c00u;
+  __device__ static __forceinline__ float lo(uint32_t w) {
+    return (float)__builtin_bit_cast(f16x2, w)[0];
+  }
+  __device__ static __forceinline__ float hi(uint32_t w) {
+    return (float)__builtin_bit_cast(f16x2, w)[1];
+  }
+  __device__ static __forceinline__ uint32_t pack(float a, float b) {
+    const f16x2 v = {(_Float16)a, (_Float16)b};
+    return __builtin_bit_cast(uint32_t, v);
+  }
+};
+
+inline bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) % n) == 0; }
+inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
+inline bool pow2(int32_t v) { return v > 0 && (v & (v - 1)) == 0; }
+inline bool page_size_ok(int32_t s) {
+  return pow2(s) && s >= PLORA_PAGE_MIN && s <= PLORA_PAGE_MAX;
+}
+inline int32_t log2_of(int32_t v) {
+  int32_t l = 0;
+  while ((1 << l) < v) ++l;
+  return l;
+}
+
+// The status of the launch just made (an error left by earlier HIP calls is
+// cleared before it by clear_error).
+inline void clear_error() { (void)hipGetLastError(); }
+inline plora_status launch_status() {
+  return hipGetLastError() == hipSuccess ? PLORA_OK : PLORA_ERR_HIP;
+}
+
+}  // namespace paged
+
+#endif  // PLORA_PAGED_DEV_H
