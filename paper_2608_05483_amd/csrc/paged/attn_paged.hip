@@ -58,30 +58,45 @@ __device__ __forceinline__ f32x16 mfma32(Fp16, u32x4 a, u32x4 b, f32x16 c) {
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
-// Valid rows of 16 keys of one page and head as a raw buffer resource: what lies
-// past them, or in a page outside the pool, reads zero and fetches nothing.
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t keys_rsrc(const AttnArgs& a, const uint16_t* x,
-                                                            const int32_t* row, int kvh, int key,
-                                                            int rows, int D) {
-  int page = -1;
-  if (rows > 0) page = row[key >> a.log_page];
+// Where 16 keys of one page and head lie, and how many bytes of them a row may
+// read: what lies past the valid rows, or in a page outside the pool, reads zero
+// through the buffer resource and fetches nothing.
+struct Cell {
+  int64_t at;
+  int bytes;
+};
+__device__ __forceinline__ int page_of(const AttnArgs& a, const int32_t* row, int key, int end) {
+  return row[min(key, end - 1) >> a.log_page];
+}
+__device__ __forceinline__ Cell cell_of(const AttnArgs& a, int page, int kvh, int key, int end,
+                                        int D) {
   page = uniform(page);
-  const bool ok = page >= 0 && page < a.n_pages;
-  const int64_t at = ok ? page * a.page_stride + kvh * a.head_stride +
-                              (int64_t)(key & ((1 << a.log_page) - 1)) * a.key_stride
-                        : 0;
-  const int bytes = ok ? ((min(rows, 16) - 1) * a.key_stride + D) * 2 : 0;
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(x) + at, 0, bytes, kRsrcWord3);
+  const bool ok = page >= 0 && page < a.n_pages && key < end;
+  page = ok ? page : 0;
+  Cell c;
+  c.at = page * a.page_stride + kvh * a.head_stride +
+         (key & ((1 << a.log_page) - 1)) * a.key_stride;
+  c.bytes = ok ? ((min(end - key, 16) - 1) * a.key_stride + D) * 2 : 0;
+  return c;
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const uint16_t* x, const Cell& c) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint16_t*>(x) + c.at, 0, c.bytes,
+                                           kRsrcWord3);
 }
 
+// POL: the cache policy.
+constexpr int kCached = 0, kOnce = 2;      // default, non-temporal
+template <int POL>
 __device__ __forceinline__ u32x4 bld16(__amdgpu_buffer_rsrc_t r, int off) {
-  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, POL));
 }
+template <int POL>
 __device__ __forceinline__ u32x2 bld8(__amdgpu_buffer_rsrc_t r, int off) {
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0));
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, POL));
 }
+template <int POL>
 __device__ __forceinline__ uint32_t bld4(__amdgpu_buffer_rsrc_t r, int off) {
-  return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
+  return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, POL);
 }
 
 // Words of 16-bit pairs (a's, b's) of the low or high halves.
@@ -167,6 +182,27 @@ __device__ __forceinline__ void careful_row(const AttnArgs& a, const Item& it, i
   }
 }
 
+// N dimensions of an output row times inv, or of a partial.
+template <class Ty, int N>
+__device__ __forceinline__ void store_out(uint16_t* out, const float (&o)[N], float inv) {
+  uint32_t w[N / 2];
+#pragma unroll
+  for (int d = 0; d < N / 2; ++d) w[d] = Ty::pack(o[2 * d] * inv, o[2 * d + 1] * inv);
+  if constexpr (N == 8) *reinterpret_cast<u32x4*>(out) = u32x4{w[0], w[1], w[2], w[3]};
+  else if constexpr (N == 4) *reinterpret_cast<u32x2*>(out) = u32x2{w[0], w[1]};
+  else *reinterpret_cast<uint32_t*>(out) = w[0];
+}
+template <int N>
+__device__ __forceinline__ void store_part(float* po, const float (&o)[N]) {
+  if constexpr (N == 2) {
+    po[0] = o[0], po[1] = o[1];
+  } else {
+#pragma unroll
+    for (int d = 0; d < N; d += 4)
+      *reinterpret_cast<f32x4*>(po + d) = f32x4{o[d], o[d + 1], o[d + 2], o[d + 3]};
+  }
+}
+
 // Items of up to 16 rows (decode: the rows are a key head's query heads times the
 // request's new tokens).  Bound by reading K and V once: 16 rows cost the matrix
 // units a twentieth of that time, so every row count up to 16 takes one tile.  The
@@ -174,7 +210,7 @@ __device__ __forceinline__ void careful_row(const AttnArgs& a, const Item& it, i
 // (K as the 16x16x32 product's rows: key n of 16, 16-byte units; V as rows of eight
 // keys), and join through LDS at the end.  The weights enter the product with V as
 // two values, hi + lo, which costs nothing here and keeps them to 16 bits.
-template <class Ty, int D>
+template <class Ty, int D, int POL>
 __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
   constexpr int kQ = D / 32;             // 16-byte units of a row, per lane
   constexpr int kV = D / 16;             // dimensions per lane
@@ -183,11 +219,54 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
   __shared__ float s_m[kWaves][kFew], s_l[kWaves][kFew];
   __shared__ int s_bad;
   const int item = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
-  if (item >= a.head->few) return;
   const Item it = a.few[item];
-  if (it.rows <= 0) return;
+  if (item >= a.head->few || it.rows <= 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
+  const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
+
+  // The loads of 32 keys; the pages of the next 32 are asked for meanwhile.  The
+  // first are under way before the query rows are known.
+  u32x4 kf[2][kQ];
+  uint32_t vw[8][kV / 2];
+  int page0, page1;
+  const auto ask = [&](int k0) {
+    page0 = page_of(a, row, k0, it.hi);
+    page1 = page_of(a, row, k0 + 16, it.hi);
+  };
+  const auto load = [&](int k0) {
+    const Cell cell[2] = {cell_of(a, page0, kvh, k0, it.hi, D),
+                          cell_of(a, page1, kvh, k0 + 16, it.hi, D)};
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const auto rk = rsrc(a.k, cell[b]);
+#pragma unroll
+      for (int j = 0; j < kQ; ++j)
+        kf[b][j] = bld16<POL>(rk, (n * a.key_stride + 32 * j + 8 * g) * 2);
+    }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const auto rv = rsrc(a.v, cell[b]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int off = ((4 * g + i) * a.key_stride + kV * n) * 2;
+        if constexpr (kV == 8) {
+          const u32x4 w = bld16<POL>(rv, off);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) vw[4 * b + i][e] = w[e];
+        } else {
+          const u32x2 w = bld8<POL>(rv, off);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) vw[4 * b + i][e] = w[e];
+        }
+      }
+    }
+    ask(k0 + kFewStep);
+  };
+  int k0 = it.lo + 32 * wv;
+  ask(k0);
+  if (k0 < it.hi) load(k0);
+
   const Row x = query_row(a, it, kvh, n);
   u32x4 qf[kQ];
 #pragma unroll
@@ -197,50 +276,17 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
 #pragma unroll
     for (int j = 0; j < kQ; ++j) qf[j] = *reinterpret_cast<const u32x4*>(q + 32 * j) ^ a.flip;
   }
-  int most = x.limit, least = n < it.rows ? x.limit : INT32_MAX;
+  int least = n < it.rows ? x.limit : INT32_MAX;
 #pragma unroll
-  for (int d = 1; d < 16; d <<= 1) {
-    most = max(most, __shfl_xor(most, d, 64));
-    least = min(least, __shfl_xor(least, d, 64));
-  }
-  most = uniform(most);
+  for (int d = 1; d < 16; d <<= 1) least = min(least, __shfl_xor(least, d, 64));
   least = uniform(least);
   if (tid == 0) s_bad = 0;
-  const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
 
   float m = -INFINITY, l = 0.f;
   f32x4 acc[kV];
 #pragma unroll
   for (int d = 0; d < kV; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int k0 = it.lo + 32 * wv; k0 < most; k0 += 32 * kWaves) {
-    u32x4 kf[2][kQ];
-    uint32_t vw[8][kV / 2];
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int key = k0 + 16 * b;
-      const auto rk = keys_rsrc(a, a.k, row, kvh, key, most - key, D);
-#pragma unroll
-      for (int j = 0; j < kQ; ++j)
-        kf[b][j] = bld16(rk, (n * a.key_stride + 32 * j + 8 * g) * 2);
-    }
-#pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int key = k0 + 16 * b;
-      const auto rv = keys_rsrc(a, a.v, row, kvh, key, most - key, D);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int off = ((4 * g + i) * a.key_stride + kV * n) * 2;
-        if constexpr (kV == 8) {
-          const u32x4 w = bld16(rv, off);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) vw[4 * b + i][e] = w[e];
-        } else {
-          const u32x2 w = bld8(rv, off);
-#pragma unroll
-          for (int e = 0; e < 2; ++e) vw[4 * b + i][e] = w[e];
-        }
-      }
-    }
+  for (; k0 < it.hi; k0 += kFewStep) {
     f32x4 s[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -283,6 +329,7 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
       acc[d] = mfma16(Ty{}, vt, ph, acc[d]);
       acc[d] = mfma16(Ty{}, vt, pl, acc[d]);
     }
+    if (k0 + kFewStep < it.hi) load(k0 + kFewStep);
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
@@ -315,19 +362,12 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
     for (int d = 0; d < kV; ++d) fine = fine && fabsf(o[d]) < INFINITY;
     if (!fine) atomicOr(&s_bad, 1 << i);
     if (it.part < 0) {
-      uint16_t* out = a.out + y.token * a.out_token + y.head * a.out_head + e;
-      const float inv = any ? 1.f / L : 0.f;
-      uint32_t w[kV / 2];
-#pragma unroll
-      for (int d = 0; d < kV / 2; ++d) w[d] = Ty::pack(o[2 * d] * inv, o[2 * d + 1] * inv);
-      if constexpr (kV == 8) *reinterpret_cast<u32x4*>(out) = u32x4{w[0], w[1], w[2], w[3]};
-      else *reinterpret_cast<u32x2*>(out) = u32x2{w[0], w[1]};
+      store_out<Ty, kV>(a.out + y.token * a.out_token + y.head * a.out_head + e, o,
+                        any ? 1.f / L : 0.f);
     } else {
       const int64_t at = ((int64_t)it.part + i) * a.kv_heads + kvh;
       if (e == 0) a.pm[at] = M, a.pl[at] = L;
-#pragma unroll
-      for (int d = 0; d < kV; d += 4)
-        *reinterpret_cast<f32x4*>(a.po + at * D + e + d) = f32x4{o[d], o[d + 1], o[d + 2], o[d + 3]};
+      store_part<kV>(a.po + at * D + e, o);
     }
   }
   __syncthreads();
@@ -347,16 +387,30 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
 // bounds the kernel, and their rounding errors average out below the output's own.
 // Bound by the matrix units and the exponentials together (for 64 keys and 32 rows
 // 1024 cycles of products, about as many of vector work).
-constexpr float kSlack = 8.f;
+constexpr float kBar = 8192.f;
+
+// Schedules n products, each fed by one read from LDS, with kAhead reads in flight.
+template <int N>
+__device__ __forceinline__ void feed() {
+  constexpr int kAhead = 6;
+  __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+  for (int i = 0; i < N - kAhead; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+}
 
 template <class Ty, int D>
 __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
   constexpr int kQ = D / 16;                // products over a row
   constexpr int kV = D / 32;                // dimensions per lane
   constexpr int kU = D / 8;                 // 16-byte units of a row
+  constexpr int kR = kU + 1;                // the same in LDS
   constexpr int kRowsPer = kNT / kU;        // K rows loaded at a time
   constexpr int kKL = kTileStep / kRowsPer; // K units per thread
-  __shared__ u32x4 s_k[2][kTileStep * kU];
+  __shared__ u32x4 s_k[2][kTileStep * kR];
   __shared__ u32x4 s_v[2][8 * kV * 32];
   __shared__ int s_most[kWaves];
   const int item = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
@@ -390,41 +444,57 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
   for (int w = 1; w < kWaves; ++w) end = max(end, s_most[w]);
   end = uniform(end);
   const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
+  const int tiles = (end - it.lo + kTileStep - 1) / kTileStep;
+  const int my = (most - it.lo + kTileStep - 1) / kTileStep;
 
-  // loaders: K rows kr + i kRowsPer, unit ku; V rows of octet o = tid / 32, kV
-  // dimensions from kV n.  The rows of one load lie in 16 keys of one page for
-  // each wavefront.
+  // Where 16 keys lie is found out for 64 times 16 keys at once, a lane each
+  // (their pages are asked for 16 steps ahead), and read from the lanes.
+  int page = 0, at_lo = 0, at_hi = 0, bytes = 0;
+  const auto ask = [&](int k0) { page = row[min(k0 + 16 * lane, end - 1) >> a.log_page]; };
+  const auto locate = [&](int k0) {
+    const int key = k0 + 16 * lane;
+    const bool ok = page >= 0 && page < a.n_pages && key < end;
+    const int64_t at = (ok ? page : 0) * a.page_stride + kvh * a.head_stride +
+                       (key & ((1 << a.log_page) - 1)) * a.key_stride;
+    at_lo = (int)at, at_hi = (int)(at >> 32);
+    bytes = ok ? ((min(end - key, 16) - 1) * a.key_stride + D) * 2 : 0;
+    ask(k0 + 1024);
+  };
+  const auto cell = [&](int j) {
+    Cell c;
+    c.at = (int64_t)(uint32_t)__builtin_amdgcn_readlane(at_lo, j) |
+           (int64_t)__builtin_amdgcn_readlane(at_hi, j) << 32;
+    c.bytes = __builtin_amdgcn_readlane(bytes, j);
+    return c;
+  };
+  // K rows kr + i kRowsPer, unit ku; V rows of octet 2 wv + h (keys 16 wv + 4 h +
+  // {0..3, 8..11}), kV dimensions from kV n.
   const int kr = tid / kU, ku = tid % kU;
   const int kg = uniform(kr >> 4), ko = kr & 15;
-  const int oh = h;                         // octet 2 wv + h: keys 16 wv + 4 h + {0..3, 8..11}
   u32x4 kreg[kKL];
   uint32_t vreg[8][(kV + 1) / 2];
-  const auto fetch = [&](int k0) {
+  const auto fetch = [&](int t) {
+    if ((t & 15) == 0) locate(it.lo + t * kTileStep);
+    const int j0 = 4 * (t & 15);
 #pragma unroll
-    for (int i = 0; i < kKL; ++i) {
-      const int key = k0 + 16 * (kg + i * (kRowsPer / 16));
-      const auto r = keys_rsrc(a, a.k, row, kvh, key, end - key, D);
-      kreg[i] = bld16(r, (ko * a.key_stride + 8 * ku) * 2);
-    }
-    const int key = k0 + 16 * wv;
-    const auto r = keys_rsrc(a, a.v, row, kvh, key, end - key, D);
+    for (int i = 0; i < kKL; ++i)
+      kreg[i] = bld16<kCached>(rsrc(a.k, cell(j0 + kg + i * (kRowsPer / 16))),
+                               (ko * a.key_stride + 8 * ku) * 2);
+    const auto r = rsrc(a.v, cell(j0 + wv));
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const int off = ((4 * oh + (i & 3) + 8 * (i >> 2)) * a.key_stride + kV * n) * 2;
+      const int off = ((4 * h + (i & 3) + 8 * (i >> 2)) * a.key_stride + kV * n) * 2;
       if constexpr (kV == 4) {
-        const u32x2 w = bld8(r, off);
+        const u32x2 w = bld8<kCached>(r, off);
         vreg[i][0] = w[0], vreg[i][1] = w[1];
       } else {
-        vreg[i][0] = bld4(r, off);
+        vreg[i][0] = bld4<kCached>(r, off);
       }
     }
   };
   const auto put = [&](int buf) {
 #pragma unroll
-    for (int i = 0; i < kKL; ++i) {
-      const int rw = kr + i * kRowsPer;
-      s_k[buf][rw * kU + (ku ^ (rw & (kU - 1)))] = kreg[i];
-    }
+    for (int i = 0; i < kKL; ++i) s_k[buf][(kr + i * kRowsPer) * kR + ku] = kreg[i];
 #pragma unroll
     for (int d = 0; d < kV; ++d) {
       u32x4 w;
@@ -434,75 +504,90 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
     }
   };
 
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, l = 0.f, bar = -1.f;
   f32x16 acc[kV];
 #pragma unroll
   for (int d = 0; d < kV; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
-  if (it.lo < end) {
-    fetch(it.lo);
+  if (tiles > 0) {
+    ask(it.lo);
+    fetch(0);
     put(0);
   }
   __syncthreads();
-  int buf = 0;
-  for (int k0 = it.lo; k0 < end; k0 += kTileStep, buf ^= 1) {
-    const bool more = k0 + kTileStep < end;
-    if (more) fetch(k0 + kTileStep);
-    if (k0 < most) {
+  for (int t = 0; t < tiles; ++t) {
+    const int buf = t & 1, k0 = it.lo + t * kTileStep;
+    if (t + 1 < tiles) fetch(t + 1);
+    if (t < my) {
+      const u32x4* kp = s_k[buf] + n * kR + h;
+      const u32x4* vp = s_v[buf] + h * kV * 32 + n;
+      // s[b][i] is key 32 b + 8 (i / 4) + 4 h + i % 4 of row n
       f32x16 s[2];
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
+      for (int b = 0; b < 2; ++b)
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[b][i] = 0.f;
-        const int rw = 32 * b + n;
 #pragma unroll
-        for (int j = 0; j < kQ; ++j)
-          s[b] = mfma32(Ty{}, s_k[buf][rw * kU + ((2 * j + h) ^ (rw & (kU - 1)))], qf[j], s[b]);
-      }
-      // s[b][i] is key 32 b + 8 (i / 4) + 4 h + i % 4 of row n
+      for (int j = 0; j < kQ; ++j)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) s[b] = mfma32(Ty{}, kp[b * 32 * kR + 2 * j], qf[j], s[b]);
+      feed<2 * kQ>();
+      __builtin_amdgcn_sched_barrier(0);
       if (k0 + kTileStep > least) {
+        const int lim = x.limit - k0 - 4 * h;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 16; ++i)
-            s[b][i] = k0 + 32 * b + 8 * (i >> 2) + 4 * h + (i & 3) < x.limit ? s[b][i] : -INFINITY;
+            s[b][i] = 32 * b + 8 * (i >> 2) + (i & 3) < lim ? s[b][i] : -INFINITY;
       }
-      float mx = -INFINITY;
+      u32x4 p[4];
+      const auto weights = [&]() {
+        const float ms = m == -INFINITY ? 0.f : m;
+        float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
-      for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
-      mx *= a.c;
-      mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-      if (__any(mx > m + kSlack)) {
-        const float mn = fmaxf(m, mx), ms = mn == -INFINITY ? 0.f : mn;
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t w = Ty::pack(exp2_(fmaf(s[b][2 * i], a.c, -ms)),
+                                        exp2_(fmaf(s[b][2 * i + 1], a.c, -ms)));
+            p[2 * b + (i >> 2)][i & 3] = w;
+            if (i & 1) sum1 = Ty::sum2(w, sum1);
+            else sum0 = Ty::sum2(w, sum0);
+          }
+        return sum0 + sum1;
+      };
+      float sum = weights();
+      if (__any(sum > bar)) {
+        float mx = m;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i] * a.c);
+        mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
+        const float ms = mx == -INFINITY ? 0.f : mx;
         const float al = exp2_(m - ms);
-        m = mn;
+        m = mx;
+        bar = m == -INFINITY ? -1.f : kBar;
         l *= al;
 #pragma unroll
         for (int d = 0; d < kV; ++d)
 #pragma unroll
           for (int i = 0; i < 16; ++i) acc[d][i] *= al;
+        sum = weights();
       }
-      const float ms = m == -INFINITY ? 0.f : m;
-      u32x4 p[4];
-#pragma unroll
-      for (int b = 0; b < 2; ++b)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float p0 = exp2_(fmaf(s[b][2 * i], a.c, -ms));
-          const float p1 = exp2_(fmaf(s[b][2 * i + 1], a.c, -ms));
-          l += p0 + p1;
-          p[2 * b + (i >> 2)][i & 3] = Ty::pack(p0, p1);
-        }
+      l += sum;
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int d = 0; d < kV; ++d)
-          acc[d] = mfma32(Ty{}, s_v[buf][((2 * b + h) * kV + d) * 32 + n], p[b], acc[d]);
+        for (int d = 0; d < kV; ++d) acc[d] = mfma32(Ty{}, vp[(2 * b * kV + d) * 32], p[b], acc[d]);
+      feed<4 * kV>();
+      __builtin_amdgcn_sched_barrier(0);
     }
-    if (more) put(buf ^ 1);
+    if (t + 1 < tiles) put(buf ^ 1);
     __syncthreads();
   }
   if (32 * wv >= it.rows) return;
@@ -516,27 +601,19 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
 #pragma unroll
     for (int i = 0; i < 16; ++i) fine = fine && fabsf(acc[d][i]) < INFINITY;
   if (mine) {
-    if (it.part < 0) {
-      uint16_t* out = a.out + x.token * a.out_token + x.head * a.out_head;
-      const float inv = any ? 1.f / l : 0.f;
+    const float inv = any ? 1.f / l : 0.f;
+    const int64_t at = ((int64_t)it.part + 32 * wv + n) * a.kv_heads + kvh;
+    if (it.part >= 0 && h == 0) a.pm[at] = m, a.pl[at] = l;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        uint16_t* o = out + kV * (8 * (i >> 2) + 4 * h + (i & 3));
-        const uint32_t w0 = Ty::pack(acc[0][i] * inv, acc[1][i] * inv);
-        if constexpr (kV == 4)
-          *reinterpret_cast<u32x2*>(o) = u32x2{w0, Ty::pack(acc[2][i] * inv, acc[3][i] * inv)};
-        else
-          *reinterpret_cast<uint32_t*>(o) = w0;
-      }
-    } else {
-      const int64_t at = ((int64_t)it.part + 32 * wv + n) * a.kv_heads + kvh;
-      if (h == 0) a.pm[at] = m, a.pl[at] = l;
+    for (int i = 0; i < 16; ++i) {
+      const int e = kV * (8 * (i >> 2) + 4 * h + (i & 3));
+      float o[kV];
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        float* o = a.po + at * D + kV * (8 * (i >> 2) + 4 * h + (i & 3));
-#pragma unroll
-        for (int d = 0; d < kV; ++d) o[d] = acc[d][i];
-      }
+      for (int d = 0; d < kV; ++d) o[d] = acc[d][i];
+      if (it.part < 0)
+        store_out<Ty, kV>(a.out + x.token * a.out_token + x.head * a.out_head + e, o, inv);
+      else
+        store_part<kV>(a.po + at * D + e, o);
     }
   }
   uint64_t bad = __ballot(mine && !fine);
@@ -548,13 +625,17 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
   }
 }
 
-// Joins a row's partials: its request's own pieces, then its prefix's.  One
-// wavefront a row; the weights of up to 64 pieces are found at once, a lane a
-// piece.  Rows that the items wrote themselves are left, rows without a key
-// get zeros.  Bound by reading the partials, or by latency.
-template <class Ty, int D>
+// Joins a row's partials: its request's own pieces, then its prefix's.  The weights
+// of up to 64 pieces are found at once, a lane a piece; the partials are then added
+// eight requests at a time.  WIDE: four wavefronts a row, a quarter of the pieces
+// each, joined in a fixed order (few rows, cut into many pieces: one request of
+// 30011 keys x 64 heads, 59 pieces: 10.0 us with a wavefront a row, @@ so); otherwise
+// a wavefront a row.  Rows that the items wrote themselves are left, rows without a
+// key get zeros.  Bound by reading the partials, or by latency.
+template <class Ty, int D, bool WIDE>
 __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
-  constexpr int kPer = D / 64;
+  constexpr int kPer = D / 64, kAt = 8;
+  __shared__ float s_o[WIDE ? kWaves : 1][64][kPer], s_m[kWaves], s_l[kWaves];
   const int t = blockIdx.x, lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
   const int b = a.req[t], heads = a.kv_heads * a.r;
   ReqInfo f{};
@@ -564,15 +645,19 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
     R0 = (t - a.q_start[b]) * a.r;
   }
   if (f.state == 2) return;
+  const int own = f.state == 1 ? f.splits : 0;
+  const int pieces = own + (f.state == 1 && f.pre_part >= 0 ? f.pre_splits : 0);
   const int end = min(heads, ((int)blockIdx.y + 1) * per);
-  for (int hd = blockIdx.y * per + wv; hd < end; hd += kWaves) {
+  for (int hd = blockIdx.y * per + (WIDE ? 0 : wv); hd < end; hd += WIDE ? 1 : kWaves) {
     const int kvh = hd / a.r, R = R0 + hd % a.r;
     uint16_t* out = a.out + t * a.out_token + hd * a.out_head + kPer * lane;
-    const int own = f.state == 1 ? f.splits : 0, pre = f.state == 1 && f.pre_part >= 0 ? f.pre_splits : 0;
-    const int pieces = own + pre;
     float M = -INFINITY, L = 0.f, o[kPer] = {};
-    for (int p0 = 0; p0 < pieces; p0 += 64) {
-      const int p = p0 + lane, n = min(64, pieces - p0);
+    const int stride = WIDE ? 64 * kWaves : 64;
+    // (WIDE: lane j of wavefront w has piece 4 j + w, so that few pieces go to all)
+    for (int p0 = 0; p0 < pieces; p0 += stride) {
+      const int p = p0 + (WIDE ? lane * kWaves + wv : lane);
+      const int left = pieces - p0;
+      const int n = min(64, WIDE ? (left - wv + kWaves - 1) / kWaves : left);
       int64_t at = 0;
       float m = -INFINITY, l = 0.f;
       if (p < pieces) {
@@ -595,13 +680,47 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
       L = (M > -INFINITY ? L * al : L) + s;
 #pragma unroll
       for (int e = 0; e < kPer; ++e) o[e] *= al;
-      for (int j = 0; j < n; ++j) {
-        const float wj = __shfl(w, j, 64);
-        const int64_t aj = __shfl(at, j, 64);
-        const float* po = a.po + aj * D + kPer * lane;
+      // eight at a time (the last repeated with a weight of 0)
+      for (int j0 = 0; j0 < n; j0 += kAt) {
+        float x[kAt][kPer];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) o[e] = fmaf(wj, po[e], o[e]);
+        for (int j = 0; j < kAt; ++j) {
+          const int64_t aj = __shfl(at, min(j0 + j, n - 1), 64);
+          const float* po = a.po + aj * D + kPer * lane;
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) x[j][e] = po[e];
+        }
+#pragma unroll
+        for (int j = 0; j < kAt; ++j) {
+          const float wj = __shfl(w, min(j0 + j, n - 1), 64);
+#pragma unroll
+          for (int e = 0; e < kPer; ++e) o[e] = j0 + j < n ? fmaf(wj, x[j][e], o[e]) : o[e];
+        }
       }
+    }
+    if constexpr (WIDE) {
+      if (lane == 0) s_m[wv] = M, s_l[wv] = L;
+#pragma unroll
+      for (int e = 0; e < kPer; ++e) s_o[wv][lane][e] = o[e];
+      __syncthreads();
+      if (wv == 0) {
+        M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+        const float ms = M == -INFINITY ? 0.f : M;
+        L = 0.f;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+          const float f2 = exp2_(s_m[w] - ms);
+          if (s_m[w] > -INFINITY || M == -INFINITY) {
+            L += s_m[w] > -INFINITY ? f2 * s_l[w] : s_l[w];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) o[e] = fmaf(f2, s_o[w][lane][e], o[e]);
+          }
+        }
+      }
+      __syncthreads();
+      if (wv != 0) continue;
     }
     const bool none = M == -INFINITY && L == 0.f;
 #pragma unroll
@@ -623,10 +742,18 @@ WsLayout ws_layout(const plora_attn_shape& s, const Bounds& b) {
   return w;
 }
 
+// Whether K and V are read with the default cache policy, so that a small cache
+// may still be in the last-level cache in the next step, or non-temporally: by the
+// size of the pool, as the host does not know the lengths (one request of 30011
+// keys on 8 heads, 123 MB: 22.6 us by default, 24.8 non-temporally; 64 x 32 x
+// 512..4096, 2.4 GB: 435 and 404; 256 requests, 0.6 GB: 128 and 124).
+constexpr int64_t kKeep = INT64_C(192) << 20;
+
 template <class Ty, int D>
-plora_status launch(const AttnArgs& a, const Bounds& b, hipStream_t stream) {
+plora_status launch(const AttnArgs& a, const Bounds& b, int64_t pool_bytes, hipStream_t stream) {
   clear_error();
-  hipLaunchKernelGGL((few_kernel<Ty, D>), dim3(b.few_cap * a.kv_heads), dim3(kNT), 0, stream, a);
+  hipLaunchKernelGGL((pool_bytes <= kKeep ? few_kernel<Ty, D, kCached> : few_kernel<Ty, D, kOnce>),
+                     dim3(b.few_cap * a.kv_heads), dim3(kNT), 0, stream, a);
   plora_status st = launch_status();
   if (st != PLORA_OK) return st;
   if (b.tile_cap > 0) {
@@ -635,10 +762,16 @@ plora_status launch(const AttnArgs& a, const Bounds& b, hipStream_t stream) {
     st = launch_status();
     if (st != PLORA_OK) return st;
   }
-  // heads of a token per work group: all, or four where the tokens are few
-  const int heads = a.kv_heads * a.r, per = a.T < 512 ? kWaves : heads;
-  hipLaunchKernelGGL((merge_kernel<Ty, D>), dim3(a.T, (heads + per - 1) / per), dim3(kNT), 0,
-                     stream, a, per);
+  // Few rows: a work group a row.  Otherwise heads of a token per work group: all,
+  // or four where the tokens are few.
+  const int heads = a.kv_heads * a.r;
+  if ((int64_t)a.T * heads <= 1024) {
+    hipLaunchKernelGGL((merge_kernel<Ty, D, true>), dim3(a.T, heads), dim3(kNT), 0, stream, a, 1);
+  } else {
+    const int per = a.T < 512 ? kWaves : heads;
+    hipLaunchKernelGGL((merge_kernel<Ty, D, false>), dim3(a.T, (heads + per - 1) / per),
+                       dim3(kNT), 0, stream, a, per);
+  }
   return launch_status();
 }
 
@@ -685,7 +818,7 @@ extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t
   const PlanLayout l = plan_layout(s, b);
   const WsLayout w = ws_layout(s, b);
   if (plan_bytes < l.bytes || ws_bytes < w.bytes) return PLORA_ERR_WORKSPACE_TOO_SMALL;
-  if ((int64_t)std::max(b.few_cap, b.tile_cap) * s.kv_heads > INT32_MAX)
+  if (((int64_t)b.few_cap + b.tile_cap) * s.kv_heads > INT32_MAX)
     return PLORA_ERR_UNSUPPORTED;
   const char* p = static_cast<const char*>(plan);
   AttnArgs a{};
@@ -723,7 +856,10 @@ extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t
   a.pm = reinterpret_cast<float*>(wp);
   a.pl = reinterpret_cast<float*>(wp + w.l);
   a.po = reinterpret_cast<float*>(wp + w.o);
+  const int64_t pool = (int64_t)c.n_pages * c.page_size * s.kv_heads * s.head_dim * 4;
   if (c.dtype == PLORA_BF16)
-    return s.head_dim == 128 ? launch<Bf16, 128>(a, b, stream) : launch<Bf16, 64>(a, b, stream);
-  return s.head_dim == 128 ? launch<Fp16, 128>(a, b, stream) : launch<Fp16, 64>(a, b, stream);
+    return s.head_dim == 128 ? launch<Bf16, 128>(a, b, pool, stream)
+                             : launch<Bf16, 64>(a, b, pool, stream);
+  return s.head_dim == 128 ? launch<Fp16, 128>(a, b, pool, stream)
+                           : launch<Fp16, 64>(a, b, pool, stream);
 }

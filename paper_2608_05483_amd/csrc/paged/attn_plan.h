@@ -17,9 +17,9 @@ constexpr int kTile = 128;
 constexpr int kFewStep = 128;
 constexpr int kTileStep = 64;
 
-// Work groups aimed at, per kind, over the whole launch (see attn_plan_kernel).
-constexpr int kFewTarget = 2048;
-constexpr int kTileTarget = 512;
+// The most pieces that cutting adds, over the whole launch (see attn_plan_kernel).
+constexpr int kFewTarget = 4096;
+constexpr int kTileTarget = 1024;
 
 // A set of query rows that read the same keys: the tokens of one request
 // ("self"), or those of a group's members (its prefix).  Rows are numbered

@@ -66,16 +66,19 @@ __device__ __forceinline__ int prefix(const PlanArgs& a, int seg) {
   return u <= 0 ? 0 : (int)(u & -(int64_t)a.page_size);
 }
 
-// How a set of rows x keys is cut.
+// How sets of rows x keys are cut.
+struct Rule {
+  int few_keys, tile_keys;   // most keys per piece
+};
 struct Cut {
   int tiles, pieces, keys;   // keys per piece
   bool few;
 };
-__device__ __forceinline__ Cut cut(int rows, int keys, int few_keys, int tile_keys) {
+__device__ __forceinline__ Cut cut(int rows, int keys, const Rule& r) {
   Cut c;
   c.few = rows <= kFew;
   c.tiles = c.few ? 1 : (rows + kTile - 1) / kTile;
-  const int most = c.few ? few_keys : tile_keys, step = c.few ? kFewStep : kTileStep;
+  const int most = c.few ? r.few_keys : r.tile_keys, step = c.few ? kFewStep : kTileStep;
   const int n = (keys - 1) / most + 1;                   // keys >= 1
   c.keys = ((keys - 1) / n + 1 + step - 1) / step * step;
   c.pieces = (keys - 1) / c.keys + 1;                    // <= n
@@ -93,20 +96,36 @@ struct Set {
   int64_t base;              // first item
 };
 
-// One work group.  Three passes over the requests: the members of the groups and
-// their tokens in group order; the work of each kind, which sets the keys per piece;
+// One work group.  Passes over the requests: the members of the groups and their
+// tokens in group order; the work of each kind, which sets the keys per piece;
 // the items (scans give each set its place, then a wavefront a set writes them).
 // Integer sums only, in a fixed order (the counts of members are sums by atomics,
 // whose order does not matter).
-// Pieces: C = work / (target / kv_heads) keys, at least kMinFew / kMinTile, so that
-// about target work groups of equal work come out; sets of fewer keys stay whole.
+//
+// Few items are cut into pieces of work / (kFewTarget / kv_heads) keys, at least
+// kMinFew: at 4096 work groups, five rounds over the chip, the last round's idle
+// ones cost little (64 requests x 32 heads x 512..4096 keys: 402 us at 768, 392 at
+// 2048, 380 at 4096), and pieces of less than 512 keys pay more for their start and
+// their partials than they gain (one request of 30011 keys on 8 heads, both
+// kernels: 42 us at 256, 33 at 512).
+// Tile items: the number of pieces changes how many rounds the chip's kTileSlots
+// work groups (two per compute unit) take, so several cuts are tried and the one
+// whose rounds x (longest piece + kTileStart) is least is taken (256 requests in 6
+// groups x 64 heads over 8, prefixes of 4000 keys: 608 work groups, two rounds, 81
+// us; 456, one, @@).
 // Once a step and bound by latency: its dependent loads and its scans.
-constexpr int kMinFew = 256, kMinTile = 256;
+constexpr int kMinFew = 512, kMinTile = 256;
+constexpr int kTileSlots = 512, kTileStart = 128;
+constexpr int kTries = 8;
+__constant__ const int kTry[kTries] = {256, 320, 384, 448, 512, 640, 768, 1024};
+static_assert(kTileTarget == 1024, "the finest cut tried bounds the items");
 
 __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
   __shared__ int64_t red[kWaves];
   __shared__ Set sets[kNT];
-  __shared__ int s_few_keys, s_tile_keys;
+  __shared__ Rule s_rule;
+  __shared__ int64_t s_items[kTries][kWaves];
+  __shared__ int s_longest[kTries][kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   int n_seg = 0, n_valid = 0;
   int64_t total;
@@ -156,32 +175,81 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
     if (tid == 0) a.moff[n_valid] = (int)carry;
     __syncthreads();
   }
-  // work of each kind: tiles x keys
-  int64_t few_work = 0, tile_work = 0;
-  const auto add = [&](int64_t rows, int keys) {
-    if (rows <= 0 || keys <= 0) return;
-    if (rows <= kFew) few_work += keys;
-    else tile_work += (rows + kTile - 1) / kTile * keys;
+  // a set's rows and keys: the groups' prefixes, then the requests' own
+  const auto set_of = [&](int i, int& rows, int& keys) {
+    int64_t n;
+    if (i < n_seg) {
+      n = a.moff[seg_begin(a, i + 1, n_valid)] - a.moff[seg_begin(a, i, n_valid)];
+      keys = prefix(a, i);
+    } else {
+      int q0, kv;
+      n = tokens(a, i - n_seg, q0, kv);
+      keys = kv - (a.shared ? a.u_len[i - n_seg] : 0);
+    }
+    n *= a.r;
+    rows = n > 0 && n <= INT32_MAX && keys > 0 ? (int)n : 0;
   };
-  for (int s = tid; s < n_seg; s += kNT)
-    add((int64_t)(a.moff[seg_begin(a, s + 1, n_valid)] - a.moff[seg_begin(a, s, n_valid)]) * a.r,
-        prefix(a, s));
-  for (int b = tid; b < a.batch; b += kNT) {
-    int q0, kv;
-    const int n = tokens(a, b, q0, kv);
-    add((int64_t)n * a.r, kv - (a.shared ? a.u_len[b] : 0));
+  const int n_sets = n_seg + a.batch;
+  // work of each kind, in tiles x keys
+  int64_t few_work = 0, tile_work = 0;
+  for (int i = tid; i < n_sets; i += kNT) {
+    int rows, keys;
+    set_of(i, rows, keys);
+    if (rows == 0) continue;
+    if (rows > kFew) tile_work += (int64_t)((rows + kTile - 1) / kTile) * keys;
+    else few_work += keys;
   }
-  const auto pieces = [&](int64_t work, int target, int least, int step) {
+  int64_t all_few, all_tile;
+  scan(few_work, red, all_few);
+  scan(tile_work, red, all_tile);
+  const auto per_piece = [&](int64_t work, int target, int least, int step) {
     const int64_t t = (target + a.kv_heads - 1) / a.kv_heads;
     const int64_t c = max((work + t - 1) / t, (int64_t)least);
     return (int)min((c + step - 1) / step * step, (int64_t)PLORA_PAGED_MAX_KEYS);
   };
-  scan(few_work, red, total);
-  if (tid == 0) s_few_keys = pieces(total, kFewTarget, kMinFew, kFewStep);
-  scan(tile_work, red, total);
-  if (tid == 0) s_tile_keys = pieces(total, kTileTarget, kMinTile, kTileStep);
+  Rule rule;
+  rule.few_keys = per_piece(all_few, kFewTarget, kMinFew, kFewStep);
+  rule.tile_keys = PLORA_PAGED_MAX_KEYS;
+  if (all_tile > 0) {
+    int64_t items[kTries] = {};
+    int longest[kTries] = {}, per[kTries];
+#pragma unroll
+    for (int k = 0; k < kTries; ++k) per[k] = per_piece(all_tile, kTry[k], kMinTile, kTileStep);
+    for (int i = tid; i < n_sets; i += kNT) {
+      int rows, keys;
+      set_of(i, rows, keys);
+      if (rows <= kFew) continue;
+#pragma unroll
+      for (int k = 0; k < kTries; ++k) {
+        const Cut c = cut(rows, keys, Rule{1, per[k]});
+        items[k] += (int64_t)c.tiles * c.pieces;
+        longest[k] = max(longest[k], c.keys);
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < kTries; ++k) {
+      for (int d = 32; d; d >>= 1) {
+        items[k] += __shfl_xor(items[k], d, 64);
+        longest[k] = max(longest[k], __shfl_xor(longest[k], d, 64));
+      }
+      if (lane == 0) s_items[k][wv] = items[k], s_longest[k][wv] = longest[k];
+    }
+    __syncthreads();
+    if (tid == 0) {
+      int64_t least = INT64_MAX;
+#pragma unroll
+      for (int k = 0; k < kTries; ++k) {
+        int64_t n = 0;
+        int len = 0;
+        for (int w = 0; w < kWaves; ++w) n += s_items[k][w], len = max(len, s_longest[k][w]);
+        const int64_t cost = (n * a.kv_heads + kTileSlots - 1) / kTileSlots * (len + kTileStart);
+        if (cost < least) least = cost, rule.tile_keys = per[k];
+      }
+    }
+  }
+  if (tid == 0) s_rule = rule;
   __syncthreads();
-  const int few_keys = s_few_keys, tile_keys = s_tile_keys;
+  rule = s_rule;
   // items: the groups' prefixes first, then the requests' own keys
   int64_t few_n = 0, tile_n = 0, part_n = 0;
   for (int pass = a.shared ? 0 : 1; pass < 2; ++pass) {
@@ -213,7 +281,7 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
       x.rows = (int)rows;
       int64_t items = 0, part = 0;
       if (rows > 0) {
-        x.c = cut(x.rows, x.hi - x.lo, few_keys, tile_keys);
+        x.c = cut(x.rows, x.hi - x.lo, rule);
         items = (int64_t)x.c.tiles * x.c.pieces;
         part = pass == 0 || u > 0 || x.c.pieces > 1 ? rows * x.c.pieces : 0;
       }
@@ -221,11 +289,10 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
       const int64_t fb = few_n + scan(x.c.few ? items : 0, red, few_total);
       const int64_t tb = tile_n + scan(x.c.few ? 0 : items, red, tile_total);
       const int64_t pb = part_n + scan(part, red, part_total);
-      // (never past the caps for lengths that agree with the shape)
-      const bool fits = (x.c.few ? fb + items <= a.few_cap : tb + items <= a.tile_cap) &&
-                        pb + part <= a.part_cap;
-      if (!fits) x.rows = 0;
       x.base = x.c.few ? fb : tb;
+      // (never past the caps for lengths that agree with the shape)
+      const int64_t cap = x.c.few ? a.few_cap : a.tile_cap;
+      if (x.base + items > cap || pb + part > a.part_cap) x.rows = 0;
       x.part = part > 0 ? (int)pb : -1;
       if (i < count && pass == 0) a.seg_part[i] = x.rows > 0 ? x.part : -1;
       if (i < count && pass == 1) {
@@ -240,7 +307,7 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
           const int all = (a.moff[seg_begin(a, s + 1, n_valid)] - t0) * a.r;
           f.pre_part = a.seg_part[s];
           f.pre_rows = all;
-          f.pre_splits = cut(all, u, few_keys, tile_keys).pieces;
+          f.pre_splits = cut(all, u, rule).pieces;
           f.pre_row = (a.place[i] - t0) * a.r;
           if (f.pre_part < 0) f.state = 0;
         }
@@ -276,7 +343,7 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
   }
   if (tid == 0)
     *a.head = {(int)min(few_n, (int64_t)a.few_cap), (int)min(tile_n, (int64_t)a.tile_cap),
-               (int)min(part_n, a.part_cap), few_keys, tile_keys};
+               (int)min(part_n, a.part_cap), rule.few_keys, rule.tile_keys};
 }
 
 }  // namespace

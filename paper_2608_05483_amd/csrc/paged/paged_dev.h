@@ -32,6 +32,11 @@ struct Bf16 {
     const bf16x2 v = {(__bf16)a, (__bf16)b};
     return __builtin_bit_cast(uint32_t, v);
   }
+  // c + the word's two values
+  __device__ static __forceinline__ float sum2(uint32_t w, float c) {
+    const bf16x2 one = {(__bf16)1.f, (__bf16)1.f};
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), one, c, false);
+  }
 };
 struct Fp16 {
   static constexpr uint32_t kExp = 0x7c00u;
@@ -44,6 +49,10 @@ struct Fp16 {
   __device__ static __forceinline__ uint32_t pack(float a, float b) {
     const f16x2 v = {(_Float16)a, (_Float16)b};
     return __builtin_bit_cast(uint32_t, v);
+  }
+  __device__ static __forceinline__ float sum2(uint32_t w, float c) {
+    const f16x2 one = {(_Float16)1.f, (_Float16)1.f};
+    return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, w), one, c, false);
   }
 };
 

@@ -9,27 +9,28 @@ namespace paged {
 namespace {
 
 constexpr int kNT = 256;
+constexpr int kBatch = 4;     // rows that a thread asks for before it uses any
 
-// One tensor of a launch: rows of (token, head), each cut into units of W
-// elements or W pairs.  units = those of one head, rot_units the first of them
-// that are turned.
+// One tensor of a launch: rows of (token, head).
 struct Part {
   const uint16_t* in;
   uint16_t* out;
-  int64_t in_token, in_head, out_token, out_head;   // out_*: pages for the cache
-  int32_t heads, units, rot_units;
-  int32_t cached;                                   // out is a pool, addressed by slot
+  int64_t in_token, in_head, out_token, out_head;   // (a pool: out_head within a page)
+  int32_t heads;
+  int32_t turned;           // else only copied
+  int32_t cached;           // out is a pool, addressed by slot
 };
 
 struct RopeArgs {
   Part part[3];
-  int32_t parts;
-  int32_t units;            // of one token, all parts
-  int32_t chunk;            // units per work group
+  int32_t parts, rows;      // rows: heads of one token, all parts
+  int32_t rows_per;         // rows per work group
+  int32_t units, rot_units; // units of a row, and how many of them turn
+  int32_t log_lanes;        // lanes of a row, a power of two
   const int32_t* pos;
   const int64_t* slot;
   const uint64_t* turns;
-  int32_t T, rot, interleaved;
+  int32_t rot, interleaved;
   float scale, sign;        // sign -1: the transposed turn
   int64_t n_slots, page_stride, key_stride;
   int32_t log_page;
@@ -54,9 +55,7 @@ union Words {
 };
 
 template <class Ty, int W>
-__device__ __forceinline__ void load(const uint16_t* p, float f[W]) {
-  Words<W> u;
-  u.v = *reinterpret_cast<const typename Unit<W>::type*>(p);
+__device__ __forceinline__ void unpack(const Words<W>& u, float f[W]) {
   if constexpr (W == 1) {
     f[0] = Ty::lo(u.h[0]);
   } else {
@@ -66,7 +65,7 @@ __device__ __forceinline__ void load(const uint16_t* p, float f[W]) {
 }
 
 template <class Ty, int W>
-__device__ __forceinline__ void store(uint16_t* p, const float f[W]) {
+__device__ __forceinline__ Words<W> pack(const float f[W]) {
   Words<W> u;
   if constexpr (W == 1) {
     u.h[0] = (uint16_t)Ty::pack(f[0], 0.f);
@@ -74,79 +73,107 @@ __device__ __forceinline__ void store(uint16_t* p, const float f[W]) {
 #pragma unroll
     for (int i = 0; i < W / 2; ++i) u.w[i] = Ty::pack(f[2 * i], f[2 * i + 1]);
   }
-  *reinterpret_cast<typename Unit<W>::type*>(p) = u.v;
+  return u;
 }
 
-// A work group takes one token (blockIdx.x) and a run of its units
-// (blockIdx.y).  cos and sin of the token's rot/2 angles are computed once, into
-// LDS (the part of a turn comes from a wrapping 64-bit product, so it is exact
-// at any position), then every unit is one load, W turns and one store: 16 bytes a lane where the layout
-// allows (W = 8).  Copies (v, elements past rot) move bits.
-// Bound by reading and writing the tensors.
+// A work group takes one token (blockIdx.x) and a run of its rows (blockIdx.y:
+// heads of q, then k, then v).  A unit is two vectors of W elements, W pairs: in the
+// half layout a thread has elements W e.. and rot/2 + W e.., otherwise 2 W e... A
+// thread keeps its unit e over all its rows, so its W cosines and sines are read
+// once, and a row is found by shifts.  cos and sin of the token's rot/2 angles are
+// computed once, into LDS (the part of a turn comes from a wrapping 64-bit product,
+// so it is exact at any position), while the first rows are on their way.  Copies
+// (v, elements past rot) move bits.
+// Bound by reading and writing the tensors (8317 tokens, 64 + 8 + 8 heads of 128:
+// @@ us; with a division for each unit and its factors read for each, 98).
 template <class Ty, int W>
 __global__ __launch_bounds__(kNT) void rope_kernel(RopeArgs a) {
   __shared__ float s_cos[PLORA_ROPE_MAX_DIM / 2], s_sin[PLORA_ROPE_MAX_DIM / 2];
   const int t = blockIdx.x, tid = threadIdx.x, half = a.rot / 2;
+  const int e = tid & ((1 << a.log_lanes) - 1), step = blockDim.x >> a.log_lanes;
+  const int end = min(a.rows, ((int)blockIdx.y + 1) * a.rows_per);
+  int row = blockIdx.y * a.rows_per + (tid >> a.log_lanes);
+  const bool turns = e < a.rot_units, idle = e >= a.units;
+  const int d0 = turns && !a.interleaved ? W * e : 2 * W * e;
+  const int d1 = turns && !a.interleaved ? half + W * e : 2 * W * e + W;
+
   const int64_t ps = a.pos[t];
-  for (int i = tid; i < half; i += kNT) {
-    const uint64_t part = (uint64_t)ps * a.turns[i];
-    // the part of a turn, signed, in half turns: [-1, 1]
-    const float x = (float)(int32_t)(part >> 32) * 0x1p-31f;
-    s_cos[i] = cospif(x) * a.scale;
-    s_sin[i] = sinpif(x) * a.scale * a.sign;
-  }
-  int64_t slot = a.slot ? a.slot[t] : 0;
+  const int64_t slot = a.slot ? a.slot[t] : 0;
   const bool kept = slot >= 0 && slot < a.n_slots;
   const int64_t page = slot >> a.log_page, key = slot - (page << a.log_page);
   const int64_t cell = page * a.page_stride + key * a.key_stride;
+  Words<W> x[kBatch], y[kBatch];
+  uint16_t* to[kBatch];
+  int o0[kBatch], o1[kBatch];
+  bool turn[kBatch];
+  const auto ask = [&]() {
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      int h = row + j * step;
+      to[j] = nullptr;
+      if (idle || h >= end) continue;
+      int n = 0;
+      if (n + 1 < a.parts && h >= a.part[0].heads) h -= a.part[0].heads, n = 1;
+      if (n + 1 < a.parts && n == 1 && h >= a.part[1].heads) h -= a.part[1].heads, n = 2;
+      const Part& p = a.part[n];
+      if (p.cached && !kept) continue;
+      const uint16_t* in = p.in + t * p.in_token + h * p.in_head;
+      to[j] = p.out + (p.cached ? cell : t * p.out_token) + h * p.out_head;
+      turn[j] = turns && p.turned;
+      o0[j] = p.turned ? d0 : 2 * W * e;
+      o1[j] = p.turned ? d1 : 2 * W * e + W;
+      x[j].v = *reinterpret_cast<const typename Unit<W>::type*>(in + o0[j]);
+      y[j].v = *reinterpret_cast<const typename Unit<W>::type*>(in + o1[j]);
+    }
+  };
+  ask();
+  for (int i = tid; i < half; i += blockDim.x) {
+    const uint64_t part = (uint64_t)ps * a.turns[i];
+    // the part of a turn, signed, in half turns: [-1, 1]
+    const float f = (float)(int32_t)(part >> 32) * 0x1p-31f;
+    s_cos[i] = cospif(f) * a.scale;
+    s_sin[i] = sinpif(f) * a.scale * a.sign;
+  }
   __syncthreads();
-  const int end = min(a.units, ((int)blockIdx.y + 1) * a.chunk);
-  for (int u0 = blockIdx.y * a.chunk + tid; u0 < end; u0 += kNT) {
-    int u = u0, n = 0;
-    while (n + 1 < a.parts && u >= a.part[n].heads * a.part[n].units) {
-      u -= a.part[n].heads * a.part[n].units;
-      ++n;
-    }
-    const Part& p = a.part[n];
-    if (p.cached && !kept) continue;
-    const int h = u / p.units, e = u - h * p.units;
-    const uint16_t* in = p.in + t * p.in_token + h * p.in_head;
-    uint16_t* out = p.out + (p.cached ? cell : t * p.out_token) + h * p.out_head;
-    if (e >= p.rot_units) {
-      const int d = (p.rot_units ? a.rot : 0) + (e - p.rot_units) * W;
-      *reinterpret_cast<typename Unit<W>::type*>(out + d) =
-          *reinterpret_cast<const typename Unit<W>::type*>(in + d);
-    } else if (!a.interleaved) {
-      float x[W], y[W], r[W], q[W];
-      load<Ty, W>(in + e * W, x);
-      load<Ty, W>(in + half + e * W, y);
+  float c[W], s[W];
 #pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float c = s_cos[e * W + i], s = s_sin[e * W + i];
-        r[i] = x[i] * c - y[i] * s;
-        q[i] = x[i] * s + y[i] * c;
-      }
-      store<Ty, W>(out + e * W, r);
-      store<Ty, W>(out + half + e * W, q);
-    } else if constexpr (W >= 2) {
-      float x[W], r[W];
-      load<Ty, W>(in + e * W, x);
+  for (int i = 0; i < W; ++i) {
+    c[i] = turns ? s_cos[W * e + i] : 1.f;
+    s[i] = turns ? s_sin[W * e + i] : 0.f;
+  }
+  while (row < end) {
 #pragma unroll
-      for (int i = 0; i < W / 2; ++i) {
-        const float c = s_cos[e * (W / 2) + i], s = s_sin[e * (W / 2) + i];
-        r[2 * i] = x[2 * i] * c - x[2 * i + 1] * s;
-        r[2 * i + 1] = x[2 * i] * s + x[2 * i + 1] * c;
+    for (int j = 0; j < kBatch; ++j) {
+      if (!to[j]) continue;
+      if (turn[j]) {
+        float f[W], g[W], p[W], q[W];
+        unpack<Ty, W>(x[j], f);
+        unpack<Ty, W>(y[j], g);
+        if (W > 1 && a.interleaved) {
+          // pairs 0 .. W/2 - 1 are in x, the others in y
+#pragma unroll
+          for (int i = 0; i < W / 2; ++i) {
+            const int k = W / 2 + i;
+            p[2 * i] = f[2 * i] * c[i] - f[2 * i + 1] * s[i];
+            p[2 * i + 1] = f[2 * i] * s[i] + f[2 * i + 1] * c[i];
+            q[2 * i] = g[2 * i] * c[k] - g[2 * i + 1] * s[k];
+            q[2 * i + 1] = g[2 * i] * s[k] + g[2 * i + 1] * c[k];
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < W; ++i) {
+            p[i] = f[i] * c[i] - g[i] * s[i];
+            q[i] = f[i] * s[i] + g[i] * c[i];
+          }
+        }
+        x[j] = pack<Ty, W>(p);
+        y[j] = pack<Ty, W>(q);
       }
-      store<Ty, W>(out + e * W, r);
-    } else {
-      // one element at a time: the pairs of this unit are 2e and 2e + 1
-      float x, y;
-      load<Ty, 1>(in + 2 * e, &x);
-      load<Ty, 1>(in + 2 * e + 1, &y);
-      const float c = s_cos[e], s = s_sin[e], r = x * c - y * s, q = x * s + y * c;
-      store<Ty, 1>(out + 2 * e, &r);
-      store<Ty, 1>(out + 2 * e + 1, &q);
+      *reinterpret_cast<typename Unit<W>::type*>(to[j] + o0[j]) = x[j].v;
+      *reinterpret_cast<typename Unit<W>::type*>(to[j] + o1[j]) = y[j].v;
     }
+    row += kBatch * step;
+    if (row < end) ask();
   }
 }
 
@@ -168,33 +195,35 @@ plora_status check(int32_t T, int32_t heads, int32_t head_dim, int32_t rot, int3
 }
 
 template <class Ty>
-void launch_type(const RopeArgs& a, int w, dim3 grid, hipStream_t stream) {
+void launch_type(const RopeArgs& a, int w, dim3 grid, int threads, hipStream_t stream) {
   auto* k = w == 8 ? rope_kernel<Ty, 8> : w == 4 ? rope_kernel<Ty, 4>
           : w == 2 ? rope_kernel<Ty, 2> : rope_kernel<Ty, 1>;
-  hipLaunchKernelGGL(k, grid, dim3(kNT), 0, stream, a);
+  hipLaunchKernelGGL(k, grid, dim3(threads), 0, stream, a);
 }
 
-// Units of the widest w that cuts every part evenly, and the launch.
-plora_status launch(RopeArgs& a, int32_t head_dim, int32_t dtype, int w, hipStream_t stream) {
-  const int turned = a.interleaved ? a.rot : a.rot / 2;     // elements that units begin in
-  while (w > 1 && (turned % w || (head_dim - a.rot) % w)) w /= 2;
-  const int rot_units = a.interleaved && w == 1 ? a.rot / 2 : turned / w;
-  a.units = 0;
-  for (int n = 0; n < a.parts; ++n) {
-    Part& p = a.part[n];
-    if (p.rot_units) p.rot_units = rot_units, p.units = rot_units + (head_dim - a.rot) / w;
-    else p.units = head_dim / w;
-    a.units += p.heads * p.units;
-  }
-  if (a.units == 0) return PLORA_OK;
-  // A token's units go to one work group, or, where the tokens alone would leave
-  // compute units idle, to one for each 256 of them
-  a.chunk = a.T < 1024 ? kNT : a.units;
-  const dim3 grid(a.T, (a.units + a.chunk - 1) / a.chunk);
-  if (grid.y > 65535) return PLORA_ERR_UNSUPPORTED;
+// Vectors of the widest w that cuts a row into whole units, and the launch.
+plora_status launch(RopeArgs& a, int32_t T, int32_t head_dim, int32_t dtype, int w,
+                    hipStream_t stream) {
+  while (w > 1 && (a.rot % (2 * w) || (head_dim - a.rot) % (2 * w))) w /= 2;
+  a.units = head_dim / (2 * w);
+  a.rot_units = a.rot / (2 * w);
+  a.log_lanes = log2_of(a.units);
+  a.rows = 0;
+  for (int n = 0; n < a.parts; ++n) a.rows += a.part[n].heads;
+  if (a.rows == 0) return PLORA_OK;
+  const int64_t lanes = (int64_t)a.rows << a.log_lanes;
+  const int threads = (int)std::min<int64_t>(kNT, (lanes + 63) / 64 * 64);
+  // A token's rows go to one work group for each kBatch passes, or, where the
+  // tokens alone would leave compute units idle, for each pass.
+  const int pass = threads >> a.log_lanes;
+  a.rows_per = T < 1024 ? pass : kBatch * pass;
+  const int blocks = (a.rows + a.rows_per - 1) / a.rows_per;
+  a.rows_per = ((a.rows + blocks - 1) / blocks + pass - 1) / pass * pass;
+  if (blocks > 65535) return PLORA_ERR_UNSUPPORTED;
   clear_error();
-  if (dtype == PLORA_BF16) launch_type<Bf16>(a, w, grid, stream);
-  else launch_type<Fp16>(a, w, grid, stream);
+  const dim3 grid(T, blocks);
+  if (dtype == PLORA_BF16) launch_type<Bf16>(a, w, grid, threads, stream);
+  else launch_type<Fp16>(a, w, grid, threads, stream);
   return launch_status();
 }
 
@@ -216,18 +245,17 @@ extern "C" plora_status plora_rope(const void* x, int64_t x_token, int64_t x_hea
   if (!aligned(x, 2) || !aligned(out, 2)) return PLORA_ERR_UNSUPPORTED;
   RopeArgs a{};
   a.part[0] = {(const uint16_t*)x, (uint16_t*)out, x_token, x_head, out_token, out_head,
-               heads, 0, rot > 0, 0};
+               heads, 1, 0};
   a.parts = 1;
   a.pos = pos;
   a.turns = turns;
-  a.T = T;
   a.rot = rot;
   a.interleaved = layout == PLORA_ROPE_INTERLEAVED;
   a.scale = scale;
   a.sign = inverse ? -1.f : 1.f;
   int w = 8;
   while (w > 1 && !(fits(w, x, x_token, x_head, 0) && fits(w, out, out_token, out_head, 0))) w /= 2;
-  return launch(a, head_dim, dtype, w, stream);
+  return launch(a, T, head_dim, dtype, w, stream);
 }
 
 extern "C" plora_status plora_rope_append(const void* q, int64_t q_token, int64_t q_head,
@@ -260,16 +288,15 @@ extern "C" plora_status plora_rope_append(const void* q, int64_t q_token, int64_
     return PLORA_ERR_UNSUPPORTED;
   RopeArgs a{};
   a.part[0] = {(const uint16_t*)q, (uint16_t*)q_out, q_token, q_head, out_token, out_head,
-               heads, 0, rot > 0, 0};
+               heads, 1, 0};
   a.part[1] = {(const uint16_t*)k, (uint16_t*)c.k, k_token, k_head, 0, c.head_stride,
-               c.kv_heads, 0, rot > 0, 1};
+               c.kv_heads, 1, 1};
   a.part[2] = {(const uint16_t*)v, (uint16_t*)c.v, v_token, v_head, 0, c.head_stride,
-               c.kv_heads, 0, 0, 1};
+               c.kv_heads, 0, 1};
   a.parts = 3;
   a.pos = pos;
   a.slot = slot;
   a.turns = turns;
-  a.T = T;
   a.rot = rot;
   a.interleaved = layout == PLORA_ROPE_INTERLEAVED;
   a.scale = scale;
@@ -284,5 +311,5 @@ extern "C" plora_status plora_rope_append(const void* q, int64_t q_token, int64_
                     fits(w, c.k, c.token_stride, c.head_stride, c.page_stride) &&
                     fits(w, c.v, c.token_stride, c.head_stride, c.page_stride)))
     w /= 2;
-  return launch(a, c.head_dim, c.dtype, w, stream);
+  return launch(a, T, c.head_dim, c.dtype, w, stream);
 }
