@@ -625,18 +625,21 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
   }
 }
 
-// Joins a row's partials: its request's own pieces, then its prefix's.  The weights
-// of up to 64 pieces are found at once, a lane a piece; the partials are then added
-// eight requests at a time.  WIDE: four wavefronts a row, a quarter of the pieces
-// each, joined in a fixed order (few rows, cut into many pieces: one request of
-// 30011 keys x 64 heads, 59 pieces: 10.0 us with a wavefront a row, @@ so); otherwise
-// a wavefront a row.  Rows that the items wrote themselves are left, rows without a
-// key get zeros.  Bound by reading the partials, or by latency.
+// Joins a row's partials: its request's own pieces, then its prefix's.  D / 4 lanes
+// a row, 64 / (D / 4) rows (heads of one token) a wavefront; the weights of up to
+// D / 4 pieces are found at once, a lane a piece, then eight partials are asked for
+// at a time.  WIDE: four wavefronts for the same rows, a quarter of the pieces each,
+// joined in a fixed order (few rows, cut into many pieces: one request of 30011 keys
+// x 64 heads, 59 pieces: 10.0 us with a wavefront a row, 5.7 so).  Rows that the
+// items wrote themselves are left, rows without a key get zeros.  Bound by reading
+// the partials, or by the latency of its chain of loads.
 template <class Ty, int D, bool WIDE>
 __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
-  constexpr int kPer = D / 64, kAt = 8;
-  __shared__ float s_o[WIDE ? kWaves : 1][64][kPer], s_m[kWaves], s_l[kWaves];
+  constexpr int kL = D / 4, kRows = 64 / kL, kAt = 8;
+  __shared__ f32x4 s_o[WIDE ? kWaves : 1][64];
+  __shared__ float s_m[WIDE ? kWaves : 1][kRows], s_l[WIDE ? kWaves : 1][kRows];
   const int t = blockIdx.x, lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+  const int e = lane % kL, sub = lane / kL;
   const int b = a.req[t], heads = a.kv_heads * a.r;
   ReqInfo f{};
   int R0 = 0;
@@ -647,27 +650,28 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
   if (f.state == 2) return;
   const int own = f.state == 1 ? f.splits : 0;
   const int pieces = own + (f.state == 1 && f.pre_part >= 0 ? f.pre_splits : 0);
+  // (WIDE: wavefront w has every fourth piece from w on)
+  const int mine = WIDE ? (pieces - wv + kWaves - 1) / kWaves : pieces;
   const int end = min(heads, ((int)blockIdx.y + 1) * per);
-  for (int hd = blockIdx.y * per + (WIDE ? 0 : wv); hd < end; hd += WIDE ? 1 : kWaves) {
-    const int kvh = hd / a.r, R = R0 + hd % a.r;
-    uint16_t* out = a.out + t * a.out_token + hd * a.out_head + kPer * lane;
-    float M = -INFINITY, L = 0.f, o[kPer] = {};
-    const int stride = WIDE ? 64 * kWaves : 64;
-    // (WIDE: lane j of wavefront w has piece 4 j + w, so that few pieces go to all)
-    for (int p0 = 0; p0 < pieces; p0 += stride) {
-      const int p = p0 + (WIDE ? lane * kWaves + wv : lane);
-      const int left = pieces - p0;
-      const int n = min(64, WIDE ? (left - wv + kWaves - 1) / kWaves : left);
+  for (int h0 = blockIdx.y * per + (WIDE ? 0 : wv * kRows); h0 < end;
+       h0 += WIDE ? kRows : kWaves * kRows) {
+    const int hd = min(h0 + sub, heads - 1), kvh = hd / a.r, R = R0 + hd % a.r;
+    float M = -INFINITY, L = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int p0 = 0; p0 < mine; p0 += kL) {
+      const int n = min(kL, mine - p0);
+      const int p = WIDE ? (p0 + e) * kWaves + wv : p0 + e;
       int64_t at = 0;
       float m = -INFINITY, l = 0.f;
-      if (p < pieces) {
+      if (e < n) {
         at = p < own ? (int64_t)f.part + (int64_t)p * f.rows + R
                      : (int64_t)f.pre_part + (int64_t)(p - own) * f.pre_rows + f.pre_row + R;
         at = at * a.kv_heads + kvh;
         m = a.pm[at], l = a.pl[at];
       }
       float mx = m;
-      for (int d = 32; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
+#pragma unroll
+      for (int d = kL / 2; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
       mx = fmaxf(mx, M);
       const float ms = mx == -INFINITY ? 0.f : mx, al = exp2_(M - ms);
       if (M == -INFINITY && mx > -INFINITY) L = 0.f;
@@ -676,57 +680,59 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
       // others; alone it makes the row NaN
       const float w = exp2_(m - ms);
       float s = m > -INFINITY ? w * l : mx > -INFINITY ? 0.f : l;
-      for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d, 64);
-      L = (M > -INFINITY ? L * al : L) + s;
 #pragma unroll
-      for (int e = 0; e < kPer; ++e) o[e] *= al;
-      // eight at a time (the last repeated with a weight of 0)
+      for (int d = kL / 2; d; d >>= 1) s += __shfl_xor(s, d, 64);
+      L = (M > -INFINITY ? L * al : L) + s;
+      o *= al;
+      // eight at a time (past the last: the last again, not added)
       for (int j0 = 0; j0 < n; j0 += kAt) {
-        float x[kAt][kPer];
+        f32x4 x[kAt];
 #pragma unroll
         for (int j = 0; j < kAt; ++j) {
-          const int64_t aj = __shfl(at, min(j0 + j, n - 1), 64);
-          const float* po = a.po + aj * D + kPer * lane;
-#pragma unroll
-          for (int e = 0; e < kPer; ++e) x[j][e] = po[e];
+          const int64_t aj = __shfl(at, min(j0 + j, n - 1), kL);
+          x[j] = *reinterpret_cast<const f32x4*>(a.po + aj * D + 4 * e);
         }
 #pragma unroll
         for (int j = 0; j < kAt; ++j) {
-          const float wj = __shfl(w, min(j0 + j, n - 1), 64);
+          const float wj = __shfl(w, min(j0 + j, n - 1), kL);
 #pragma unroll
-          for (int e = 0; e < kPer; ++e) o[e] = j0 + j < n ? fmaf(wj, x[j][e], o[e]) : o[e];
+          for (int i = 0; i < 4; ++i) o[i] = j0 + j < n ? fmaf(wj, x[j][i], o[i]) : o[i];
         }
       }
     }
     if constexpr (WIDE) {
-      if (lane == 0) s_m[wv] = M, s_l[wv] = L;
-#pragma unroll
-      for (int e = 0; e < kPer; ++e) s_o[wv][lane][e] = o[e];
+      if (e == 0) s_m[wv][sub] = M, s_l[wv][sub] = L;
+      s_o[wv][lane] = o;
       __syncthreads();
       if (wv == 0) {
-        M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
-        const float ms = M == -INFINITY ? 0.f : M;
-        L = 0.f;
+        M = s_m[0][sub];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) o[e] = 0.f;
+        for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][sub]);
+        L = 0.f;
+        o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-          const float f2 = exp2_(s_m[w] - ms);
-          if (s_m[w] > -INFINITY || M == -INFINITY) {
-            L += s_m[w] > -INFINITY ? f2 * s_l[w] : s_l[w];
-#pragma unroll
-            for (int e = 0; e < kPer; ++e) o[e] = fmaf(f2, s_o[w][lane][e], o[e]);
+          const float mw = s_m[w][sub], lw = s_l[w][sub];
+          if (mw == -INFINITY) {
+            if (M == -INFINITY) L += lw;
+            continue;
           }
+          const float g = exp2_(mw - M);
+          L = fmaf(g, lw, L);
+          const f32x4 x = s_o[w][lane];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[i] = fmaf(g, x[i], o[i]);
         }
       }
       __syncthreads();
       if (wv != 0) continue;
     }
+    if (h0 + sub >= end) continue;
     const bool none = M == -INFINITY && L == 0.f;
+    float v[4];
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) o[e] = none ? 0.f : o[e] / L;
-    if constexpr (kPer == 2) *reinterpret_cast<uint32_t*>(out) = Ty::pack(o[0], o[1]);
-    else *out = (uint16_t)Ty::pack(o[0], 0.f);
+    for (int i = 0; i < 4; ++i) v[i] = none ? 0.f : o[i] / L;
+    store_out<Ty, 4>(a.out + t * a.out_token + hd * a.out_head + 4 * e, v, 1.f);
   }
 }
 
@@ -762,13 +768,14 @@ plora_status launch(const AttnArgs& a, const Bounds& b, int64_t pool_bytes, hipS
     st = launch_status();
     if (st != PLORA_OK) return st;
   }
-  // Few rows: a work group a row.  Otherwise heads of a token per work group: all,
-  // or four where the tokens are few.
-  const int heads = a.kv_heads * a.r;
+  // Few rows: a work group for what otherwise is a wavefront's.  Else heads of a
+  // token per work group: all, or one pass where the tokens are few.
+  const int heads = a.kv_heads * a.r, rows = 256 / D;
   if ((int64_t)a.T * heads <= 1024) {
-    hipLaunchKernelGGL((merge_kernel<Ty, D, true>), dim3(a.T, heads), dim3(kNT), 0, stream, a, 1);
+    hipLaunchKernelGGL((merge_kernel<Ty, D, true>), dim3(a.T, (heads + rows - 1) / rows),
+                       dim3(kNT), 0, stream, a, rows);
   } else {
-    const int per = a.T < 512 ? kWaves : heads;
+    const int per = a.T < 512 ? kWaves * rows : heads;
     hipLaunchKernelGGL((merge_kernel<Ty, D, false>), dim3(a.T, (heads + per - 1) / per),
                        dim3(kNT), 0, stream, a, per);
   }
