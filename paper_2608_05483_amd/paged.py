@@ -15,8 +15,9 @@ from __future__ import annotations
 import ctypes
 import math
 
-from . import plora as _plora
-from .plora import PloraError, lib, plora_segments  # noqa: F401
+import torch
+
+from .plora import PLORA_OK, PloraError, lib, plora_segments
 
 BF16, FP16 = 0, 1
 HALF, INTERLEAVED = 0, 1
@@ -78,27 +79,45 @@ def _declare(L) -> None:
 _declare(lib)
 
 
+# (int16: bf16 bits, as in plora)
+_CODE = {torch.bfloat16: BF16, torch.int16: BF16, torch.float16: FP16}
+_I32, _I64 = torch.int32, torch.int64
+_current = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream(stream, t) -> int:
+    """The stream given, or the current one of the tensor's device."""
+    if stream is not None:
+        return int(stream.cuda_stream)
+    if _current is not None:
+        return _current(t.get_device())
+    return int(torch.cuda.current_stream(t.device).cuda_stream)
+
+
+def _ok(fn: str, status: int) -> None:
+    if status != PLORA_OK:
+        raise PloraError(fn, status)
+
+
 def _dtype(t) -> int:
-    import torch
-    if t.dtype in (torch.bfloat16, torch.int16):     # int16: bf16 bits, as in plora
-        return BF16
-    if t.dtype == torch.float16:
-        return FP16
-    raise TypeError(f"bf16 or fp16 tensor expected, got {t.dtype}")
+    code = _CODE.get(t.dtype)
+    if code is None:
+        raise TypeError(f"bf16 or fp16 tensor expected, got {t.dtype}")
+    return code
 
 
-def _heads(name: str, t, dtype: int | None = None):
+def _heads(name: str, t, dtype: int):
     """Pointer, token stride and head stride of a [T, heads, dim] tensor."""
-    if t.dim() != 3 or (t.shape[2] > 1 and t.stride(2) != 1):
+    s = t.stride()
+    if len(s) != 3 or (s[2] != 1 and t.shape[2] > 1):
         raise ValueError(f"{name}: a [T, heads, dim] tensor with contiguous dim expected")
-    if dtype is not None and _dtype(t) != dtype:
-        raise TypeError(f"{name}: has another type than the cache")
-    return t.data_ptr(), t.stride(0), t.stride(1)
+    if _CODE.get(t.dtype) != dtype:
+        raise TypeError(f"{name}: has another type than expected")
+    return t.data_ptr(), s[0], s[1]
 
 
-def _ints(name: str, t, dtype: str, n: int):
-    import torch
-    if t.dtype != getattr(torch, dtype) or t.numel() < n or not t.is_contiguous():
+def _ints(name: str, t, dtype, n: int):
+    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor of at least {n} entries expected")
     return t.data_ptr()
 
@@ -118,11 +137,11 @@ class KVCache:
         self.struct = plora_kv_cache(self.n_pages, self.page_size, self.kv_heads, self.head_dim,
                                      self.dtype, 0, k.data_ptr(), v.data_ptr(), k.stride(0),
                                      k.stride(1), k.stride(2))
+        self.ref = ctypes.byref(self.struct)
 
     @classmethod
     def empty(cls, n_pages: int, page_size: int, kv_heads: int, head_dim: int, dtype=None,
               device="cuda"):
-        import torch
         shape = (n_pages, kv_heads, page_size, head_dim)
         mk = lambda: torch.zeros(shape, dtype=dtype or torch.bfloat16, device=device)
         return cls(mk(), mk())
@@ -134,11 +153,10 @@ class Step:
 
     def __init__(self, batch: int, T: int, page_size: int, max_pages: int, device="cuda",
                  table=None):
-        import torch
         self.batch, self.T, self.page_size, self.max_pages = batch, T, page_size, max_pages
         i32 = dict(dtype=torch.int32, device=device)
         self.table = table if table is not None else torch.zeros((batch, max_pages), **i32)
-        _ints("table", self.table, "int32", batch * max_pages)
+        _ints("table", self.table, _I32, batch * max_pages)
         self.q_start = torch.zeros(batch + 1, **i32)
         self.kv_len = torch.zeros(batch, **i32)
         self.pos = torch.zeros(T, **i32)
@@ -149,6 +167,7 @@ class Step:
                                     self.q_start.data_ptr(), self.kv_len.data_ptr(),
                                     self.pos.data_ptr(), self.req.data_ptr(),
                                     self.slot.data_ptr(), self.meta.data_ptr())
+        self.ref = ctypes.byref(self.struct)
 
 
 class AttnPlan:
@@ -157,9 +176,10 @@ class AttnPlan:
 
     def __init__(self, step: Step, heads: int, kv_heads: int, head_dim: int, max_q: int,
                  shared: bool = False, device="cuda"):
-        import torch
         self.shape = plora_attn_shape(step.batch, step.T, heads, kv_heads, head_dim, max_q,
                                       int(shared), 0)
+        self.ref = ctypes.byref(self.shape)
+        self.q_shape = (step.T, heads, head_dim)
         u8 = dict(dtype=torch.uint8, device=device)
         self.plan = torch.zeros(attn_plan_bytes(self.shape), **u8)
         self.ws = torch.empty(attn_paged_workspace_bytes(self.shape), **u8)
@@ -179,68 +199,72 @@ def attn_paged_workspace_bytes(shape: plora_attn_shape) -> int:
 def kv_plan(past, n_new, free_pages, free_head, free_next, step: Step, stream=None) -> None:
     """past, n_new int32 [batch]; free_pages int32, handed out from entry
     free_head[0] on; free_next[0] is the entry after."""
-    _plora._ok("plora_kv_plan", lib.plora_kv_plan(
-        _ints("past", past, "int32", step.batch), _ints("n_new", n_new, "int32", step.batch),
-        _ints("free_pages", free_pages, "int32", 0), free_pages.numel(),
-        _ints("free_head", free_head, "int32", 1), _ints("free_next", free_next, "int32", 1),
-        ctypes.byref(step.struct), _plora._stream(stream)))
+    n = step.batch
+    _ok("plora_kv_plan", lib.plora_kv_plan(
+        _ints("past", past, _I32, n), _ints("n_new", n_new, _I32, n),
+        _ints("free_pages", free_pages, _I32, 0), free_pages.numel(),
+        _ints("free_head", free_head, _I32, 1), _ints("free_next", free_next, _I32, 1),
+        step.ref, _stream(stream, past)))
 
 
 def rope(x, pos, turns, out, layout: str = "half", scale: float = 1.0, inverse: bool = False,
          stream=None) -> None:
     """x, out [T, heads, dim]; rot = 2 turns.numel() elements of each head turn;
     inverse gives the input's gradient from the output's."""
-    T, H, D = x.shape
     if out.shape != x.shape:
         raise ValueError("out: x's shape expected")
     dt = _dtype(x)
-    px, xt, xh = _heads("x", x)
+    px, xt, xh = _heads("x", x, dt)
     po, ot, oh = _heads("out", out, dt)
-    _plora._ok("plora_rope", lib.plora_rope(
-        px, xt, xh, _ints("pos", pos, "int32", T), _ints("turns", turns, "int64", 0), T, H, D,
-        2 * turns.numel(), _LAYOUT[layout], scale, int(inverse), dt, po, ot, oh,
-        _plora._stream(stream)))
+    T, H, D = x.shape
+    _ok("plora_rope", lib.plora_rope(
+        px, xt, xh, _ints("pos", pos, _I32, T), _ints("turns", turns, _I64, 0), T, H, D,
+        2 * turns.numel(), _LAYOUT[layout], scale, inverse, dt, po, ot, oh, _stream(stream, x)))
 
 
 def rope_append(q, k, v, pos, slot, turns, cache: KVCache, q_out, layout: str = "half",
                 scale: float = 1.0, stream=None) -> None:
     """q, q_out [T, heads, dim], k, v [T, kv_heads, dim], pos int32 [T], slot
     int64 [T]: q turned into q_out, k turned into the cache, v stored there."""
-    T, H = q.shape[:2]
-    D, KH = cache.head_dim, cache.kv_heads
-    if q.shape[2] != D or q_out.shape != q.shape or tuple(k.shape) != (T, KH, D) or \
+    dt = cache.dtype
+    pq, qt, qh = _heads("q", q, dt)
+    pk, kt, kh = _heads("k", k, dt)
+    pv, vt, vh = _heads("v", v, dt)
+    po, ot, oh = _heads("q_out", q_out, dt)
+    T, H, D = q.shape
+    if D != cache.head_dim or q_out.shape != q.shape or k.shape != (T, cache.kv_heads, D) or \
             v.shape != k.shape:
         raise ValueError("q, k, v, q_out: shapes do not fit each other and the cache")
-    _plora._ok("plora_rope_append", lib.plora_rope_append(
-        *_heads("q", q, cache.dtype), *_heads("k", k, cache.dtype), *_heads("v", v, cache.dtype),
-        _ints("pos", pos, "int32", T), _ints("slot", slot, "int64", T),
-        _ints("turns", turns, "int64", 0), T, H, 2 * turns.numel(), _LAYOUT[layout], scale,
-        ctypes.byref(cache.struct), *_heads("q_out", q_out, cache.dtype),
-        _plora._stream(stream)))
+    _ok("plora_rope_append", lib.plora_rope_append(
+        pq, qt, qh, pk, kt, kh, pv, vt, vh, _ints("pos", pos, _I32, T),
+        _ints("slot", slot, _I64, T), _ints("turns", turns, _I64, 0), T, H, 2 * turns.numel(),
+        _LAYOUT[layout], scale, cache.ref, po, ot, oh, _stream(stream, q)))
 
 
 def attn_plan(step: Step, plan: AttnPlan, segs=None, prefix_len=None, stream=None) -> None:
     """segs: the batch's groups (plora.Segments filled by plora.segment from a
     group id per request); prefix_len int32 [n_groups]."""
-    n = segs.n_adapters if segs is not None else 0
-    _plora._ok("plora_attn_plan", lib.plora_attn_plan(
-        ctypes.byref(step.struct), ctypes.byref(plan.shape),
-        ctypes.byref(segs.struct) if segs is not None else None,
-        _ints("prefix_len", prefix_len, "int32", n) if prefix_len is not None else None, n,
-        plan.plan.data_ptr(), plan.plan.numel(), _plora._stream(stream)))
+    groups, lens, n = None, None, 0
+    if segs is not None:
+        groups, n = ctypes.byref(segs.struct), segs.n_adapters
+    if prefix_len is not None:
+        lens = _ints("prefix_len", prefix_len, _I32, n)
+    _ok("plora_attn_plan", lib.plora_attn_plan(
+        step.ref, plan.ref, groups, lens, n, plan.plan.data_ptr(), plan.plan.numel(),
+        _stream(stream, plan.plan)))
 
 
 def attn_paged(q, cache: KVCache, step: Step, plan: AttnPlan, scale: float, out,
                stream=None) -> None:
     """q, out [T, heads, head_dim]."""
-    s = plan.shape
-    if tuple(q.shape) != (s.T, s.heads, s.head_dim) or out.shape != q.shape:
+    dt = cache.dtype
+    pq, qt, qh = _heads("q", q, dt)
+    po, ot, oh = _heads("out", out, dt)
+    if q.shape != plan.q_shape or out.shape != plan.q_shape:
         raise ValueError("q, out: the plan's [T, heads, head_dim] expected")
-    _plora._ok("plora_attn_paged", lib.plora_attn_paged(
-        *_heads("q", q, cache.dtype), ctypes.byref(cache.struct), ctypes.byref(step.struct),
-        ctypes.byref(s), scale, plan.plan.data_ptr(), plan.plan.numel(),
-        *_heads("out", out, cache.dtype), plan.ws.data_ptr(), plan.ws.numel(),
-        _plora._stream(stream)))
+    _ok("plora_attn_paged", lib.plora_attn_paged(
+        pq, qt, qh, cache.ref, step.ref, plan.ref, scale, plan.plan.data_ptr(),
+        plan.plan.numel(), po, ot, oh, plan.ws.data_ptr(), plan.ws.numel(), _stream(stream, q)))
 
 
 # ---- the rotation's frequencies ---------------------------------------------------
@@ -257,7 +281,6 @@ def rope_turns(rot: int, base: float = 10000.0, scaling: str = "none", factor: f
     fewer than low turns over the original context, keeps those that make more
     than high, and blends between in proportion to the turns."""
     import numpy as np
-    import torch
     if rot < 0 or rot % 2 or base <= 0 or factor <= 0:
         raise ValueError("rot: even and not negative, base and factor: positive")
     if scaling == "base" and rot > 2:
