@@ -6,8 +6,8 @@
 // straight from those registers: the matrix instruction's output layout gives a
 // lane groups of four keys, and since a product may sum its keys in any order, V
 // is brought into the same order.  No weight crosses a lane.  V^T needs, for one
-// dimension, eight keys in a lane: the lane loads eight rows and transposes the
-// 16-bit block in its own registers.
+// dimension, eight keys in a lane: few_kernel loads eight rows and transposes the
+// 16-bit block in the lane's own registers, tile_kernel reads columns from LDS.
 // The scores are kept times scale log2(e), so a weight is one exp2 of one fma.
 
 #include <cmath>
@@ -376,42 +376,65 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
 }
 
 // Items of up to 128 rows: prompts, and prefixes that many rows share.  A wavefront
-// has 32 rows; K and V go through LDS, 64 keys at a time, two buffers: the next
-// keys are loaded into registers while the present ones are used, and stored after.
-// K rows keep their order with 16-byte units turned by the row number (a read takes
-// one unit of 32 rows); V is transposed by its loader, so a lane reads the eight
-// keys of one dimension as one unit.  A row's maximum is only raised when a score
-// passes it by more than 8 (in powers of two), so the output is rarely rescaled:
-// weights are at most 2^8 then, of the same relative precision.
-// The weights enter the product with V rounded once to the type: this product
-// bounds the kernel, and their rounding errors average out below the output's own.
-// Bound by the matrix units and the exponentials together (for 64 keys and 32 rows
-// 1024 cycles of products, about as many of vector work).
+// has 32 rows; K and V go through LDS, 64 keys at a time, two buffers, loaded there
+// directly: the next keys are on their way while the present ones are used.  Rows
+// stay rows in LDS, their 16-byte units turned by the row number, which the loaders'
+// addresses do: for K by row mod 16, so that a read of one unit of 32 rows meets no
+// bank twice; for V in steps of four units, for reads that transpose (16 lanes take
+// 16 dimensions of four keys and each gets one dimension's four).
+// The weights are formed against the row's present maximum before it is known
+// whether that still stands: it is only raised, the output rescaled and the weights
+// formed again, if a lane's sum of 32 passes 2^13.  So no maximum is looked for in
+// most steps; no weight passes 2^13 then, which either type holds with its full
+// precision.  The weights are summed as rounded to the type, which they are for the
+// product with V: its rounding errors average out below the output's own, and a
+// second product for the rest would add half to the work that bounds the kernel.
+// Bound by the matrix units and what they cannot hide: for 64 keys and 32 rows 32
+// products (1024 cycles), 64 vector instructions and 32 exponentials (512), 64 reads
+// of LDS (about 600).  64 keys x 128 rows, two work groups on every compute unit:
+// 2.1 us a step, of which products alone take 1.4 (1029 TFLOP/s where K and V come
+// from L2; 16 requests of 256 tokens behind 8192 keys, 32 heads).  With the keys
+// through registers into LDS and V transposed there 2.4 us; with a maximum each step
+// and a sum by additions 2.7; eight wavefronts a work group in two phases, one
+// side's products beside the other's exponentials, 2.8.
 constexpr float kBar = 8192.f;
 
-// Schedules n products, each fed by one read from LDS, with kAhead reads in flight.
-template <int N>
+// Schedules n products, each fed by r reads from LDS, four products' reads ahead.
+template <int N, int R>
 __device__ __forceinline__ void feed() {
-  constexpr int kAhead = 6;
-  __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+  constexpr int kAhead = 4;
+  __builtin_amdgcn_sched_group_barrier(0x100, R * kAhead, 0);
 #pragma unroll
   for (int i = 0; i < N - kAhead; ++i) {
     __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
   }
   __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
 }
 
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4* lds_quad;
+typedef __attribute__((address_space(3))) void* lds_ptr;
+
+// Four 16-bit values of a lane's column: lane i of each 16 names the address of four
+// values of row i / 4 (columns 4 (i % 4)..), and gets column i of the four rows.
+__device__ __forceinline__ u32x2 read_columns(const uint16_t* p) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_quad)p));
+}
+
+// Waits for this wavefront's loads (those into LDS among them).
+__device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
+
 template <class Ty, int D>
 __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
   constexpr int kQ = D / 16;                // products over a row
-  constexpr int kV = D / 32;                // dimensions per lane
+  constexpr int kV = D / 32;                // tiles of the output's dimensions
   constexpr int kU = D / 8;                 // 16-byte units of a row
-  constexpr int kR = kU + 1;                // the same in LDS
   constexpr int kRowsPer = kNT / kU;        // K rows loaded at a time
   constexpr int kKL = kTileStep / kRowsPer; // K units per thread
-  __shared__ u32x4 s_k[2][kTileStep * kR];
-  __shared__ u32x4 s_v[2][8 * kV * 32];
+  // (buffers by name: reads of one are seen not to meet the loads into the other)
+  __shared__ u32x4 s_k0[kTileStep * kU], s_k1[kTileStep * kU];
+  __shared__ u32x4 s_v0[kTileStep * kU], s_v1[kTileStep * kU];
   __shared__ int s_most[kWaves];
   const int item = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
   if (item >= a.head->tiles) return;
@@ -467,44 +490,31 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
     c.bytes = __builtin_amdgcn_readlane(bytes, j);
     return c;
   };
-  // K rows kr + i kRowsPer, unit ku; V rows of octet 2 wv + h (keys 16 wv + 4 h +
-  // {0..3, 8..11}), kV dimensions from kV n.
+  const auto turn_v = [](int rw) { return (D == 128 ? rw & 3 : (rw >> 1) & 1) << 2; };
+  // Rows kr + i kRowsPer, place ku of the row in LDS; a load's rows lie in 16 keys of
+  // one page.
   const int kr = tid / kU, ku = tid % kU;
   const int kg = uniform(kr >> 4), ko = kr & 15;
-  u32x4 kreg[kKL];
-  uint32_t vreg[8][(kV + 1) / 2];
-  const auto fetch = [&](int t) {
+  const int off_k = (ko * a.key_stride + 8 * (ku ^ (kr & (kU - 1)))) * 2;
+  const int off_v = (ko * a.key_stride + 8 * (ku ^ turn_v(kr))) * 2;
+  const auto fetch = [&](int t, u32x4* sk, u32x4* sv) {
     if ((t & 15) == 0) locate(it.lo + t * kTileStep);
     const int j0 = 4 * (t & 15);
 #pragma unroll
-    for (int i = 0; i < kKL; ++i)
-      kreg[i] = bld16<kCached>(rsrc(a.k, cell(j0 + kg + i * (kRowsPer / 16))),
-                               (ko * a.key_stride + 8 * ku) * 2);
-    const auto r = rsrc(a.v, cell(j0 + wv));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int off = ((4 * h + (i & 3) + 8 * (i >> 2)) * a.key_stride + kV * n) * 2;
-      if constexpr (kV == 4) {
-        const u32x2 w = bld8<kCached>(r, off);
-        vreg[i][0] = w[0], vreg[i][1] = w[1];
-      } else {
-        vreg[i][0] = bld4<kCached>(r, off);
-      }
-    }
-  };
-  const auto put = [&](int buf) {
-#pragma unroll
-    for (int i = 0; i < kKL; ++i) s_k[buf][(kr + i * kRowsPer) * kR + ku] = kreg[i];
-#pragma unroll
-    for (int d = 0; d < kV; ++d) {
-      u32x4 w;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = zip(vreg[2 * i][d / 2], vreg[2 * i + 1][d / 2], d & 1);
-      s_v[buf][((2 * wv + h) * kV + d) * 32 + n] = w;
+    for (int i = 0; i < kKL; ++i) {
+      const Cell c = cell(j0 + kg + i * (kRowsPer / 16));
+      const int to = (i * kRowsPer + wv * (kRowsPer / kWaves)) * kU;
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(a.k, c), (lds_ptr)(sk + to), 16, off_k, 0, 0,
+                                               0);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc(a.v, c), (lds_ptr)(sv + to), 16, off_v, 0, 0,
+                                               0);
     }
   };
 
-  float m = -INFINITY, l = 0.f, bar = -1.f;
+  // (a row that sees none of the item's keys never asks for a maximum, a row without
+  // one yet always)
+  const float first = x.limit > it.lo ? -1.f : INFINITY;
+  float m = -INFINITY, l = 0.f, bar = first;
   f32x16 acc[kV];
 #pragma unroll
   for (int d = 0; d < kV; ++d)
@@ -512,16 +522,19 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
     for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
   if (tiles > 0) {
     ask(it.lo);
-    fetch(0);
-    put(0);
+    fetch(0, s_k0, s_v0);
+    loads_done();
   }
   __syncthreads();
-  for (int t = 0; t < tiles; ++t) {
-    const int buf = t & 1, k0 = it.lo + t * kTileStep;
-    if (t + 1 < tiles) fetch(t + 1);
+  const auto step = [&](int t, const u32x4* sk, const u32x4* sv, u32x4* nk, u32x4* nv) {
+    const int k0 = it.lo + t * kTileStep;
+    if (t + 1 < tiles) fetch(t + 1, nk, nv);
     if (t < my) {
-      const u32x4* kp = s_k[buf] + n * kR + h;
-      const u32x4* vp = s_v[buf] + h * kV * 32 + n;
+      const u32x4* kp = sk + n * kU;
+      const int kx = h ^ (n & (kU - 1));
+      const int vi = lane & 15, vrow = 4 * h + (vi >> 2);
+      const uint16_t* vp = reinterpret_cast<const uint16_t*>(sv) + vrow * D +
+                           16 * (lane >> 4 & 1) + 4 * (vi & 3);
       // s[b][i] is key 32 b + 8 (i / 4) + 4 h + i % 4 of row n
       f32x16 s[2];
       __builtin_amdgcn_sched_barrier(0);
@@ -532,8 +545,9 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
 #pragma unroll
       for (int j = 0; j < kQ; ++j)
 #pragma unroll
-        for (int b = 0; b < 2; ++b) s[b] = mfma32(Ty{}, kp[b * 32 * kR + 2 * j], qf[j], s[b]);
-      feed<2 * kQ>();
+        for (int b = 0; b < 2; ++b)
+          s[b] = mfma32(Ty{}, kp[b * 32 * kU + (kx ^ (2 * j))], qf[j], s[b]);
+      feed<2 * kQ, 1>();
       __builtin_amdgcn_sched_barrier(0);
       if (k0 + kTileStep > least) {
         const int lim = x.limit - k0 - 4 * h;
@@ -570,7 +584,7 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
         const float ms = mx == -INFINITY ? 0.f : mx;
         const float al = exp2_(m - ms);
         m = mx;
-        bar = m == -INFINITY ? -1.f : kBar;
+        bar = m == -INFINITY ? first : kBar;
         l *= al;
 #pragma unroll
         for (int d = 0; d < kV; ++d)
@@ -583,18 +597,26 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
 #pragma unroll
       for (int b = 0; b < 4; ++b)
 #pragma unroll
-        for (int d = 0; d < kV; ++d) acc[d] = mfma32(Ty{}, vp[(2 * b * kV + d) * 32], p[b], acc[d]);
-      feed<4 * kV>();
+        for (int d = 0; d < kV; ++d) {
+          const uint16_t* v = vp + 16 * b * D + ((32 * d) ^ (turn_v(vrow) * 8));
+          const u32x2 v0 = read_columns(v), v1 = read_columns(v + 8 * D);
+          acc[d] = mfma32(Ty{}, u32x4{v0[0], v0[1], v1[0], v1[1]}, p[b], acc[d]);
+        }
+      feed<4 * kV, 2>();
       __builtin_amdgcn_sched_barrier(0);
     }
-    if (t + 1 < tiles) put(buf ^ 1);
+    loads_done();
     __syncthreads();
+  };
+  for (int t = 0; t < tiles; t += 2) {
+    step(t, s_k0, s_v0, s_k1, s_v1);
+    if (t + 1 < tiles) step(t + 1, s_k1, s_v1, s_k0, s_v0);
   }
   if (32 * wv >= it.rows) return;
   l += __shfl_xor(l, 32, 64);
   const bool any = x.limit > it.lo;
   if (m == -INFINITY && any) l = NAN;
-  // acc[d][i] is the output's dimension kV (8 (i / 4) + 4 h + i % 4) + d of row n
+  // acc[d][i] is the output's dimension 32 d + 8 (i / 4) + 4 h + i % 4 of row n
   bool fine = true;
 #pragma unroll
   for (int d = 0; d < kV; ++d)
@@ -605,16 +627,16 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
     const int64_t at = ((int64_t)it.part + 32 * wv + n) * a.kv_heads + kvh;
     if (it.part >= 0 && h == 0) a.pm[at] = m, a.pl[at] = l;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int e = kV * (8 * (i >> 2) + 4 * h + (i & 3));
-      float o[kV];
+    for (int d = 0; d < kV; ++d)
 #pragma unroll
-      for (int d = 0; d < kV; ++d) o[d] = acc[d][i];
-      if (it.part < 0)
-        store_out<Ty, kV>(a.out + x.token * a.out_token + x.head * a.out_head + e, o, inv);
-      else
-        store_part<kV>(a.po + at * D + e, o);
-    }
+      for (int i = 0; i < 16; i += 4) {
+        const int e = 32 * d + 2 * i + 4 * h;
+        const float o[4] = {acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+        if (it.part < 0)
+          store_out<Ty, 4>(a.out + x.token * a.out_token + x.head * a.out_head + e, o, inv);
+        else
+          store_part<4>(a.po + at * D + e, o);
+      }
   }
   uint64_t bad = __ballot(mine && !fine);
   bad = (bad | bad >> 32) & 0xffffffffu;
