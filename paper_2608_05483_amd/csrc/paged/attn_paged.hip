@@ -210,31 +210,32 @@ __device__ __forceinline__ void store_part(float* po, const float (&o)[N]) {
 // (K as the 16x16x32 product's rows: key n of 16, 16-byte units; V as rows of eight
 // keys), and join through LDS at the end.  The weights enter the product with V as
 // two values, hi + lo, which costs nothing here and keeps them to 16 bits.
-template <class Ty, int D, int POL>
-__global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
+struct FewShared {
+  float m[kWaves][kFew], l[kWaves][kFew];
+  int bad, most[kWaves];
+};
+template <class Ty, int D, int POL, bool AHEAD>
+__device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int kvh,
+                                         FewShared& sh, f32x4* o01, f32x4* o23) {
   constexpr int kQ = D / 32;             // 16-byte units of a row, per lane
   constexpr int kV = D / 16;             // dimensions per lane
-  constexpr int kPad = D + 4;
-  __shared__ float s_o[kWaves][kFew][kPad];
-  __shared__ float s_m[kWaves][kFew], s_l[kWaves][kFew];
-  __shared__ int s_bad;
-  const int item = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
-  const Item it = a.few[item];
-  if (item >= a.head->few || it.rows <= 0) return;
+  if (it.rows <= 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   const int n = lane & 15, g = lane >> 4;
   const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
 
   // The loads of 32 keys; the pages of the next 32 are asked for meanwhile.  The
   // first are under way before the query rows are known.
-  u32x4 kf[2][kQ];
-  uint32_t vw[8][kV / 2];
+  struct Keys {
+    u32x4 k[2][kQ];
+    uint32_t v[8][kV / 2];
+  } ka, kb;
   int page0, page1;
   const auto ask = [&](int k0) {
     page0 = page_of(a, row, k0, it.hi);
     page1 = page_of(a, row, k0 + 16, it.hi);
   };
-  const auto load = [&](int k0) {
+  const auto load = [&](Keys& x, int k0) {
     const Cell cell[2] = {cell_of(a, page0, kvh, k0, it.hi, D),
                           cell_of(a, page1, kvh, k0 + 16, it.hi, D)};
 #pragma unroll
@@ -242,7 +243,7 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
       const auto rk = rsrc(a.k, cell[b]);
 #pragma unroll
       for (int j = 0; j < kQ; ++j)
-        kf[b][j] = bld16<POL>(rk, (n * a.key_stride + 32 * j + 8 * g) * 2);
+        x.k[b][j] = bld16<POL>(rk, (n * a.key_stride + 32 * j + 8 * g) * 2);
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -253,11 +254,11 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
         if constexpr (kV == 8) {
           const u32x4 w = bld16<POL>(rv, off);
 #pragma unroll
-          for (int e = 0; e < 4; ++e) vw[4 * b + i][e] = w[e];
+          for (int e = 0; e < 4; ++e) x.v[4 * b + i][e] = w[e];
         } else {
           const u32x2 w = bld8<POL>(rv, off);
 #pragma unroll
-          for (int e = 0; e < 2; ++e) vw[4 * b + i][e] = w[e];
+          for (int e = 0; e < 2; ++e) x.v[4 * b + i][e] = w[e];
         }
       }
     }
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
   };
   int k0 = it.lo + 32 * wv;
   ask(k0);
-  if (k0 < it.hi) load(k0);
+  if (k0 < it.hi) load(ka, k0);
 
   const Row x = query_row(a, it, kvh, n);
   u32x4 qf[kQ];
@@ -280,19 +281,19 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
 #pragma unroll
   for (int d = 1; d < 16; d <<= 1) least = min(least, __shfl_xor(least, d, 64));
   least = uniform(least);
-  if (tid == 0) s_bad = 0;
+  if (tid == 0) sh.bad = 0;
 
   float m = -INFINITY, l = 0.f;
   f32x4 acc[kV];
 #pragma unroll
   for (int d = 0; d < kV; ++d) acc[d] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (; k0 < it.hi; k0 += kFewStep) {
+  const auto use = [&](const Keys& y, int k0) {
     f32x4 s[2];
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       s[b] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < kQ; ++j) s[b] = mfma16(Ty{}, kf[b][j], qf[j], s[b]);
+      for (int j = 0; j < kQ; ++j) s[b] = mfma16(Ty{}, y.k[b][j], qf[j], s[b]);
     }
     float t[8];
 #pragma unroll
@@ -323,44 +324,69 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
     for (int d = 0; d < kV; ++d) {
       u32x4 vt;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) vt[i] = zip(vw[2 * i][d / 2], vw[2 * i + 1][d / 2], d & 1);
+      for (int i = 0; i < 4; ++i) vt[i] = zip(y.v[2 * i][d / 2], y.v[2 * i + 1][d / 2], d & 1);
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[d][i] *= al;
       acc[d] = mfma16(Ty{}, vt, ph, acc[d]);
       acc[d] = mfma16(Ty{}, vt, pl, acc[d]);
     }
-    if (k0 + kFewStep < it.hi) load(k0 + kFewStep);
+  };
+  if constexpr (AHEAD) {
+    while (k0 < it.hi) {
+      if (k0 + kFewStep < it.hi) load(kb, k0 + kFewStep);
+      use(ka, k0);
+      k0 += kFewStep;
+      if (k0 >= it.hi) break;
+      if (k0 + kFewStep < it.hi) load(ka, k0 + kFewStep);
+      use(kb, k0);
+      k0 += kFewStep;
+    }
+  } else {
+    for (; k0 < it.hi; k0 += kFewStep) {
+      use(ka, k0);
+      if (k0 + kFewStep < it.hi) load(ka, k0 + kFewStep);
+    }
   }
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
-  if (g == 0) s_m[wv][n] = m, s_l[wv][n] = l;
-  // acc[d][i] is the output's dimension kV (4 g + i) + d of row n
+  if (g == 0) sh.m[wv][n] = m, sh.l[wv][n] = l;
+  // acc[d][i] is the output's dimension kV (4 g + i) + d of row n; in LDS the
+  // 16-byte units of a row are turned by its number
+  const auto place = [&](int w, int r, int unit) {
+    return (w < 2 ? o01 : o23) + ((w & 1) * kFew + r) * (D / 4) + (unit ^ r);
+  };
 #pragma unroll
   for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int d = 0; d < kV; ++d) s_o[wv][n][kV * (4 * g + i) + d] = acc[d][i];
+    for (int d = 0; d < kV; d += 4)
+      *place(wv, n, (kV * (4 * g + i) + d) / 4) =
+          f32x4{acc[d][i], acc[d + 1][i], acc[d + 2][i], acc[d + 3][i]};
   __syncthreads();
   const int i = tid >> 4, e = (tid & 15) * kV;
   if (i < it.rows) {
     const Row y = query_row(a, it, kvh, i);
-    float M = s_m[0][i];
+    float M = sh.m[0][i];
 #pragma unroll
-    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][i]);
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sh.m[w][i]);
     const float Ms = M == -INFINITY ? 0.f : M;
     float L = 0.f, o[kV] = {};
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) {
-      const float f = exp2_(s_m[w][i] - Ms);
-      L = fmaf(f, s_l[w][i], L);
+      const float f = exp2_(sh.m[w][i] - Ms);
+      L = fmaf(f, sh.l[w][i], L);
 #pragma unroll
-      for (int d = 0; d < kV; ++d) o[d] = fmaf(f, s_o[w][i][e + d], o[d]);
+      for (int d = 0; d < kV; d += 4) {
+        const f32x4 v = *place(w, i, (e + d) / 4);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) o[d + c] = fmaf(f, v[c], o[d + c]);
+      }
     }
     const bool any = y.limit > it.lo;
     if (M == -INFINITY && any) L = NAN;
     bool fine = true;
 #pragma unroll
     for (int d = 0; d < kV; ++d) fine = fine && fabsf(o[d]) < INFINITY;
-    if (!fine) atomicOr(&s_bad, 1 << i);
+    if (!fine) atomicOr(&sh.bad, 1 << i);
     if (it.part < 0) {
       store_out<Ty, kV>(a.out + y.token * a.out_token + y.head * a.out_head + e, o,
                         any ? 1.f / L : 0.f);
@@ -372,7 +398,19 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
   }
   __syncthreads();
   for (int b = wv; b < it.rows; b += kWaves)
-    if (s_bad >> b & 1) careful_row<Ty, D>(a, it, kvh, b);
+    if (sh.bad >> b & 1) careful_row<Ty, D>(a, it, kvh, b);
+}
+
+// The few items of a step that can have no others.
+template <class Ty, int D, int POL>
+__global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
+  __shared__ f32x4 o01[2 * kFew * D / 4], o23[2 * kFew * D / 4];
+  __shared__ FewShared sh;
+  // (the grid covers the items' cap, so the item may be read beside their number)
+  const int item = blockIdx.x / a.kv_heads;
+  const Item it = a.few[item];
+  if (item >= a.head->few) return;
+  few_item<Ty, D, POL, false>(a, it, blockIdx.x % a.kv_heads, sh, o01, o23);
 }
 
 // Items of up to 128 rows: prompts, and prefixes that many rows share.  A wavefront
@@ -426,19 +464,14 @@ __device__ __forceinline__ u32x2 read_columns(const uint16_t* p) {
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
 template <class Ty, int D>
-__global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
+__device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int kvh,
+                                          int* s_most, u32x4* s_k0, u32x4* s_k1, u32x4* s_v0,
+                                          u32x4* s_v1) {
   constexpr int kQ = D / 16;                // products over a row
   constexpr int kV = D / 32;                // tiles of the output's dimensions
   constexpr int kU = D / 8;                 // 16-byte units of a row
   constexpr int kRowsPer = kNT / kU;        // K rows loaded at a time
   constexpr int kKL = kTileStep / kRowsPer; // K units per thread
-  // (buffers by name: reads of one are seen not to meet the loads into the other)
-  __shared__ u32x4 s_k0[kTileStep * kU], s_k1[kTileStep * kU];
-  __shared__ u32x4 s_v0[kTileStep * kU], s_v1[kTileStep * kU];
-  __shared__ int s_most[kWaves];
-  const int item = blockIdx.x / a.kv_heads, kvh = blockIdx.x % a.kv_heads;
-  if (item >= a.head->tiles) return;
-  const Item it = a.tile[item];
   if (it.rows <= 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
@@ -647,6 +680,34 @@ __global__ __launch_bounds__(kNT, 2) void tile_kernel(AttnArgs a) {
   }
 }
 
+// Both kinds of items in one launch, in turn in proportion to their numbers, so that
+// the compute units hold work groups of both at once: the one kind is bound by
+// reading, the other by the matrix units (256 requests in 6 groups, @@ us in two
+// launches, @@ so).  Eight work groups in a row are of one kind, so that a head's
+// items, which share K and V, stay on one XCD where the key heads are a multiple
+// of 8.
+template <class Ty, int D, int POL>
+__global__ __launch_bounds__(kNT, 2) void items_kernel(AttnArgs a) {
+  // (buffers by name: reads of one are seen not to meet the loads into the other)
+  __shared__ u32x4 s_k0[kTileStep * D / 8], s_k1[kTileStep * D / 8];
+  __shared__ u32x4 s_v0[kTileStep * D / 8], s_v1[kTileStep * D / 8];
+  __shared__ FewShared sh;
+  static_assert(sizeof(s_k0) == 2 * kFew * D * sizeof(float), "two wavefronts' outputs");
+  const uint32_t turn = blockIdx.x >> 3, in = blockIdx.x & 7;
+  const uint64_t rate = a.head->tile_rate;
+  const uint32_t t0 = (uint32_t)(turn * rate >> 32), t1 = (uint32_t)((turn + 1) * rate >> 32);
+  const bool tile = t1 > t0;
+  const uint32_t index = (tile ? t0 : turn - t0) * 8 + in, item = index / a.kv_heads;
+  const int kvh = index % a.kv_heads;
+  // (the work groups behind the last item would pass the lists' ends)
+  if (item >= (uint32_t)(tile ? a.head->tiles : a.head->few)) return;
+  if (tile)
+    tile_item<Ty, D>(a, a.tile[item], kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
+  else
+    few_item<Ty, D, POL, true>(a, a.few[item], kvh, sh, reinterpret_cast<f32x4*>(s_k0),
+                               reinterpret_cast<f32x4*>(s_k1));
+}
+
 // Joins a row's partials: its request's own pieces, then its prefix's.  D / 4 lanes
 // a row, 64 / (D / 4) rows (heads of one token) a wavefront; the weights of up to
 // D / 4 pieces are found at once, a lane a piece, then eight partials are asked for
@@ -777,19 +838,24 @@ WsLayout ws_layout(const plora_attn_shape& s, const Bounds& b) {
 // 512..4096, 2.4 GB: 435 and 404; 256 requests, 0.6 GB: 128 and 124).
 constexpr int64_t kKeep = INT64_C(192) << 20;
 
+// Work groups for the caps of both kinds, in eights.
+int64_t item_blocks(const Bounds& b, int32_t kv_heads) {
+  const int64_t few = (int64_t)b.few_cap * kv_heads, tiles = (int64_t)b.tile_cap * kv_heads;
+  return ((few + 7) / 8 + (tiles + 7) / 8) * 8;
+}
+
 template <class Ty, int D>
 plora_status launch(const AttnArgs& a, const Bounds& b, int64_t pool_bytes, hipStream_t stream) {
+  const bool keep = pool_bytes <= kKeep;
   clear_error();
-  hipLaunchKernelGGL((pool_bytes <= kKeep ? few_kernel<Ty, D, kCached> : few_kernel<Ty, D, kOnce>),
-                     dim3(b.few_cap * a.kv_heads), dim3(kNT), 0, stream, a);
+  if (b.tile_cap > 0)
+    hipLaunchKernelGGL((keep ? items_kernel<Ty, D, kCached> : items_kernel<Ty, D, kOnce>),
+                       dim3(item_blocks(b, a.kv_heads)), dim3(kNT), 0, stream, a);
+  else
+    hipLaunchKernelGGL((keep ? few_kernel<Ty, D, kCached> : few_kernel<Ty, D, kOnce>),
+                       dim3(b.few_cap * a.kv_heads), dim3(kNT), 0, stream, a);
   plora_status st = launch_status();
   if (st != PLORA_OK) return st;
-  if (b.tile_cap > 0) {
-    hipLaunchKernelGGL((tile_kernel<Ty, D>), dim3(b.tile_cap * a.kv_heads), dim3(kNT), 0, stream,
-                       a);
-    st = launch_status();
-    if (st != PLORA_OK) return st;
-  }
   // Few rows: a work group for what otherwise is a wavefront's.  Else heads of a
   // token per work group: all, or one pass where the tokens are few.
   const int heads = a.kv_heads * a.r, rows = 256 / D;
@@ -847,7 +913,7 @@ extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t
   const PlanLayout l = plan_layout(s, b);
   const WsLayout w = ws_layout(s, b);
   if (plan_bytes < l.bytes || ws_bytes < w.bytes) return PLORA_ERR_WORKSPACE_TOO_SMALL;
-  if (((int64_t)b.few_cap + b.tile_cap) * s.kv_heads > INT32_MAX)
+  if (item_blocks(b, s.kv_heads) > INT32_MAX)
     return PLORA_ERR_UNSUPPORTED;
   const char* p = static_cast<const char*>(plan);
   AttnArgs a{};

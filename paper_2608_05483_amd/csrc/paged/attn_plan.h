@@ -95,6 +95,8 @@ struct PlanHeader {
   int32_t few, tiles;          // items
   int32_t part_rows;
   int32_t few_keys, tile_keys; // keys per piece
+  int32_t reserved;
+  uint64_t tile_rate;          // eights of tile work groups among all, times 2^32
 };
 
 inline bool shape_ok(const plora_attn_shape& s) {

@@ -341,9 +341,19 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
       part_n += part_total;
     }
   }
-  if (tid == 0)
-    *a.head = {(int)min(few_n, (int64_t)a.few_cap), (int)min(tile_n, (int64_t)a.tile_cap),
-               (int)min(part_n, a.part_cap), rule.few_keys, rule.tile_keys};
+  if (tid == 0) {
+    PlanHeader h{};
+    h.few = (int)min(few_n, (int64_t)a.few_cap);
+    h.tiles = (int)min(tile_n, (int64_t)a.tile_cap);
+    h.part_rows = (int)min(part_n, a.part_cap);
+    h.few_keys = rule.few_keys;
+    h.tile_keys = rule.tile_keys;
+    // rounded up: all tiles have come by the last work group, at most one an eight
+    const uint64_t few8 = ((uint64_t)h.few * a.kv_heads + 7) / 8;
+    const uint64_t tile8 = ((uint64_t)h.tiles * a.kv_heads + 7) / 8;
+    h.tile_rate = tile8 ? ((tile8 << 32) + few8 + tile8 - 1) / (few8 + tile8) : 0;
+    *a.head = h;
+  }
 }
 
 }  // namespace
