@@ -701,10 +701,11 @@ __global__ __launch_bounds__(kNT, 2) void items_kernel(AttnArgs a) {
   const int kvh = index % a.kv_heads;
   // (the work groups behind the last item would pass the lists' ends)
   if (item >= (uint32_t)(tile ? a.head->tiles : a.head->few)) return;
+  const Item it = (tile ? a.tile : a.few)[item];
   if (tile)
-    tile_item<Ty, D>(a, a.tile[item], kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
+    tile_item<Ty, D>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
   else
-    few_item<Ty, D, POL, true>(a, a.few[item], kvh, sh, reinterpret_cast<f32x4*>(s_k0),
+    few_item<Ty, D, POL, true>(a, it, kvh, sh, reinterpret_cast<f32x4*>(s_k0),
                                reinterpret_cast<f32x4*>(s_k1));
 }
 
