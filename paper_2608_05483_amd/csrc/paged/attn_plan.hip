@@ -112,7 +112,7 @@ struct Set {
 // work groups (two per compute unit) take, so several cuts are tried and the one
 // whose rounds x (longest piece + kTileStart) is least is taken (256 requests in 6
 // groups x 64 heads over 8, prefixes of 4000 keys: 608 work groups, two rounds, 81
-// us; 456, one, @@).
+// us; 456, one, 64; the tile items alone).
 // Once a step and bound by latency: its dependent loads and its scans.
 constexpr int kMinFew = 512, kMinTile = 256;
 constexpr int kTileSlots = 512, kTileStart = 128;
