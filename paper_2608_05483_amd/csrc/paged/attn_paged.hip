@@ -21,7 +21,6 @@ constexpr int kNT = 256;
 constexpr int kWaves = kNT / 64;
 constexpr int kRsrcWord3 = 0x00020000;    // raw buffer, 32-bit data format (gfx9 family)
 typedef int i32x4 __attribute__((ext_vector_type(4)));
-typedef int i32x2 __attribute__((ext_vector_type(2)));
 
 struct AttnArgs {
   const uint16_t *q, *k, *v;
@@ -914,7 +913,7 @@ extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t
   const PlanLayout l = plan_layout(s, b);
   const WsLayout w = ws_layout(s, b);
   if (plan_bytes < l.bytes || ws_bytes < w.bytes) return PLORA_ERR_WORKSPACE_TOO_SMALL;
-  if (item_blocks(b, s.kv_heads) > INT32_MAX)
+  if (item_blocks(b, s.kv_heads) > (int64_t)(UINT32_MAX / kNT))   // threads of a launch
     return PLORA_ERR_UNSUPPORTED;
   const char* p = static_cast<const char*>(plan);
   AttnArgs a{};

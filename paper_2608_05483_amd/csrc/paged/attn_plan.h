@@ -21,6 +21,10 @@ constexpr int kTileStep = 64;
 constexpr int kFewTarget = 4096;
 constexpr int kTileTarget = 1024;
 
+// Requests for which the plan's kernel keeps what it needs in LDS, and its arrays.
+constexpr int kHere = 1024;
+constexpr int kKeptArrays = 12;
+
 // A set of query rows that read the same keys: the tokens of one request
 // ("self"), or those of a group's members (its prefix).  Rows are numbered
 // (token, head in the key head's group), token first; an item is a run of a
@@ -75,9 +79,10 @@ inline Bounds bounds(const plora_attn_shape& s) {
   return b;
 }
 
-// Words of the plan: a header, the items, the gathered tokens, the requests.
+// Bytes of the plan: a header, the items, the gathered tokens, the requests, and what
+// the plan's kernel keeps of many requests.
 struct PlanLayout {
-  size_t few, tile, order, req, scratch, bytes;
+  size_t few, tile, order, req, kept, bytes;
 };
 inline PlanLayout plan_layout(const plora_attn_shape& s, const Bounds& b) {
   PlanLayout l{};
@@ -85,10 +90,8 @@ inline PlanLayout plan_layout(const plora_attn_shape& s, const Bounds& b) {
   l.tile = l.few + align256((size_t)b.few_cap * sizeof(Item));
   l.order = l.tile + align256((size_t)b.tile_cap * sizeof(Item));
   l.req = l.order + align256(s.shared ? (size_t)s.T * 4 : 0);
-  l.scratch = l.req + align256((size_t)s.batch * sizeof(ReqInfo));
-  // per request: its shared keys, its place among the gathered tokens, its group;
-  // per group: members, keys
-  l.bytes = l.scratch + align256(s.shared ? (size_t)(s.batch + 1) * 5 * 4 : 0);
+  l.kept = l.req + align256((size_t)s.batch * sizeof(ReqInfo));
+  l.bytes = l.kept + align256(s.batch > kHere ? (size_t)(s.batch + 1) * kKeptArrays * 4 : 0);
   return l;
 }
 struct PlanHeader {

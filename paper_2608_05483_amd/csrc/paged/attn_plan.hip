@@ -21,86 +21,133 @@ struct PlanArgs {
   Item *few, *tile;
   int32_t* order;
   ReqInfo* info;
-  int32_t *u_len, *place, *seg_of, *moff, *seg_part;   // [batch + 1] each, groups only
-  int32_t few_cap, tile_cap;
-  int64_t part_cap;
+  int32_t* kept;             // kKeptArrays x [batch + 1], steps of more than kHere requests
+  int32_t few_cap, tile_cap, part_cap;
 };
 
-// Exclusive scan of one value a thread over the work group; total is the sum.
-__device__ __forceinline__ int64_t scan(int64_t x, int64_t* red, int64_t& total) {
+// What is found out once about each request and each group, in LDS or, for steps
+// of more than kHere requests, in the plan.
+struct Kept {
+  // requests: new tokens (0: none, or the step left it out), the first, keys, keys
+  // that it shares, its group, the place of its first token in the groups' order
+  int32_t *n, *q0, *kv, *u, *seg, *place;
+  // entries of perm: tokens of members before it
+  int32_t* moff;
+  // groups: first entry of perm, keys of the prefix, who could share (then the
+  // prefix's first partial row), its pieces, its first member
+  int32_t *begin, *pre, *part, *splits, *req;
+};
+static_assert(sizeof(Kept) == kKeptArrays * sizeof(int32_t*), "");
+
+// A value moved over lanes, 0 where none comes (all lanes active).
+template <int CTRL, int ROWS, class V>
+__device__ __forceinline__ V moved(V x) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(
+        V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
+  } else {
+    const i32x2 w = __builtin_bit_cast(i32x2, x);
+    const i32x2 y = {__builtin_amdgcn_update_dpp(0, w[0], CTRL, ROWS, 0xf, false),
+                     __builtin_amdgcn_update_dpp(0, w[1], CTRL, ROWS, 0xf, false)};
+    return __builtin_bit_cast(V, y);
+  }
+}
+// Inclusive scan over a wavefront: within rows of 16 lanes, then over the rows.
+template <class V, class Op>
+__device__ __forceinline__ V wave_scan(V x, Op op) {
+  x = op(x, moved<0x111, 0xf>(x));
+  x = op(x, moved<0x112, 0xf>(x));
+  x = op(x, moved<0x114, 0xf>(x));
+  x = op(x, moved<0x118, 0xf>(x));
+  x = op(x, moved<0x142, 0xa>(x));
+  return op(x, moved<0x143, 0xc>(x));
+}
+// Counts, none below 0, are kept to 2^30, above every cap.
+constexpr uint32_t kMany = 1u << 30;
+struct Add {
+  template <class V>
+  __device__ V operator()(V a, V b) const { return a + b; }
+};
+struct AddCount {
+  __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return min(a + b, kMany); }
+};
+struct Max {
+  __device__ int operator()(int a, int b) const { return max(a, b); }
+};
+
+// Exclusive scans of N counts a thread over the work group, from carry on, which
+// then holds the sums.
+template <int N>
+__device__ __forceinline__ void scan(uint32_t (&x)[N], uint32_t (&carry)[N],
+                                     uint32_t (&red)[kWaves][N]) {
+  const AddCount add;
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  int64_t inc = x;
+  uint32_t inc[N];
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int64_t y = __shfl_up(inc, d, 64);
-    if (lane >= d) inc += y;
-  }
-  if (lane == 63) red[wv] = inc;
-  __syncthreads();
-  int64_t before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wv) before += red[w];
-    all += red[w];
+  for (int i = 0; i < N; ++i) {
+    inc[i] = wave_scan(x[i], add);
+    if (lane == 63) red[wv][i] = inc[i];
   }
   __syncthreads();
-  total = all;
-  return before + inc - x;
-}
-
-// A request's new tokens, 0 if it has none or the step left it out.
-__device__ __forceinline__ int tokens(const PlanArgs& a, int b, int& q0, int& kv) {
-  q0 = a.q_start[b];
-  kv = a.kv_len[b];
-  const int q1 = a.q_start[b + 1];
-  if (q0 < 0 || q0 >= q1 || q1 > a.T || a.req[q0] != b) return 0;
-  const int n = q1 - q0;
-  return n > a.max_q || kv < n || kv > a.max_keys ? 0 : n;
-}
-
-// The whole pages of a group's prefix, in keys.
-__device__ __forceinline__ int prefix(const PlanArgs& a, int seg) {
-  const int g = a.seg_id[seg];
-  if (g < 0 || g >= a.n_groups) return 0;
-  const int64_t u = min((int64_t)a.prefix_len[g], a.max_keys);
-  return u <= 0 ? 0 : (int)(u & -(int64_t)a.page_size);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    uint32_t before = carry[i], all = carry[i];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const uint32_t y = red[w][i];
+      if (w < wv) before = add(before, y);
+      all = add(all, y);
+    }
+    // (what is before this lane; exact below kMany, and not below it otherwise)
+    x[i] = add(before, inc[i] < kMany ? inc[i] - x[i] : kMany);
+    carry[i] = all;
+  }
+  __syncthreads();
 }
 
 // How sets of rows x keys are cut.
-struct Rule {
-  int few_keys, tile_keys;   // most keys per piece
-};
 struct Cut {
   int tiles, pieces, keys;   // keys per piece
   bool few;
 };
-__device__ __forceinline__ Cut cut(int rows, int keys, const Rule& r) {
+__device__ __forceinline__ Cut cut(int rows, int keys, int few_keys, int tile_keys) {
   Cut c;
   c.few = rows <= kFew;
   c.tiles = c.few ? 1 : (rows + kTile - 1) / kTile;
-  const int most = c.few ? r.few_keys : r.tile_keys, step = c.few ? kFewStep : kTileStep;
-  const int n = (keys - 1) / most + 1;                   // keys >= 1
-  c.keys = ((keys - 1) / n + 1 + step - 1) / step * step;
-  c.pieces = (keys - 1) / c.keys + 1;                    // <= n
+  const uint32_t last = keys - 1;                        // keys >= 1
+  const uint32_t n = last / (uint32_t)(c.few ? few_keys : tile_keys) + 1;
+  const uint32_t step = c.few ? kFewStep : kTileStep;
+  c.keys = (int)((last / n + step) & -step);
+  c.pieces = (int)(last / (uint32_t)c.keys + 1);         // <= n
   return c;
 }
-
-// First place of a segment in perm.
-__device__ __forceinline__ int seg_begin(const PlanArgs& a, int s, int n_valid) {
-  return min(max(a.seg_ptr[s], 0), n_valid);
-}
+static_assert(pow2(kFewStep) && pow2(kTileStep), "");
 
 struct Set {
   int32_t tok, rows, req, lo, hi, part, gathered;
   Cut c;
-  int64_t base;              // first item
+  int32_t base, items;       // first item, items that the list has room for
 };
 
-// One work group.  Passes over the requests: the members of the groups and their
-// tokens in group order; the work of each kind, which sets the keys per piece;
-// the items (scans give each set its place, then a wavefront a set writes them).
-// Integer sums only, in a fixed order (the counts of members are sums by atomics,
-// whose order does not matter).
+__device__ __forceinline__ void emit(const PlanArgs& a, const Set& x, int j, int tile,
+                                     int piece) {
+  Item it;
+  it.tok = x.tok;
+  it.row = tile * kTile;
+  it.rows = min(x.rows - it.row, kTile);                 // none if the set did not fit
+  it.req = x.req;
+  it.lo = x.lo + piece * x.c.keys;
+  it.hi = min(x.hi, it.lo + x.c.keys);
+  it.part = x.part < 0 ? -1 : x.part + piece * x.rows + it.row;
+  it.gathered = x.gathered;
+  (x.c.few ? a.few : a.tile)[x.base + j] = it;
+}
+
+// One work group.  Passes over the requests: what is known of each; the members of
+// the groups and their tokens in group order; the work of each kind, which sets the
+// keys per piece; the items (a scan gives each set its place; its thread writes up
+// to kOwn items, a wavefront a set's where there are more).  Sums of whole numbers
+// only, or of as many in 64-bit floats, which hold them: no order changes them.
 //
 // Few items are cut into pieces of work / (kFewTarget / kv_heads) keys, at least
 // kMinFew: at 4096 work groups, five rounds over the chip, the last round's idle
@@ -109,245 +156,271 @@ struct Set {
 // their partials than they gain (one request of 30011 keys on 8 heads, both
 // kernels: 42 us at 256, 33 at 512).
 // Tile items: the number of pieces changes how many rounds the chip's kTileSlots
-// work groups (two per compute unit) take, so several cuts are tried and the one
-// whose rounds x (longest piece + kTileStart) is least is taken (256 requests in 6
-// groups x 64 heads over 8, prefixes of 4000 keys: 608 work groups, two rounds, 81
-// us; 456, one, 64; the tile items alone).
-// Once a step and bound by latency: its dependent loads and its scans.
+// work groups (two per compute unit) take, so several cuts are tried, a wavefront
+// each, and the one whose rounds x (longest piece + kTileStart) is least is taken
+// (256 requests in 6 groups x 64 heads over 8, prefixes of 4000 keys: 608 work
+// groups, two rounds, 81 us; 456, one, 64; the tile items alone).
+//
+// Once a step and bound by latency: dependent loads, barriers, and code that is
+// fetched for the first time.
 constexpr int kMinFew = 512, kMinTile = 256;
 constexpr int kTileSlots = 512, kTileStart = 128;
-constexpr int kTries = 8;
+constexpr int kTries = kWaves;
 __constant__ const int kTry[kTries] = {256, 320, 384, 448, 512, 640, 768, 1024};
 static_assert(kTileTarget == 1024, "the finest cut tried bounds the items");
+constexpr int kOwn = 8;
+
+// Keys per piece so that work is cut into target / kv_heads pieces.  (Both are whole
+// numbers below 2^53 and the result, where it is not cut off, below 2^30: the
+// division in 64-bit floats rounds to a whole number only where it is one.)
+__device__ __forceinline__ int per_piece(double work, int target, int kv_heads, int least,
+                                         int step) {
+  const int t = (target + kv_heads - 1) / kv_heads;
+  const double c = min(max(ceil(work / t), (double)least), (double)PLORA_PAGED_MAX_KEYS);
+  return min(((int)c + step - 1) & -step, PLORA_PAGED_MAX_KEYS);
+}
 
 __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
-  __shared__ int64_t red[kWaves];
-  __shared__ Set sets[kNT];
-  __shared__ Rule s_rule;
-  __shared__ int64_t s_items[kTries][kWaves];
-  __shared__ int s_longest[kTries][kWaves];
+  __shared__ int32_t s_kept[kKeptArrays * (kHere + 1)];
+  __shared__ Set s_sets[kNT];
+  __shared__ int s_keys[kNT], s_tiles[kNT], s_big[kNT], s_bigs;
+  __shared__ uint32_t red1[kWaves][1], red3[kWaves][3];
+  __shared__ double s_work[kWaves][2];
+  __shared__ int64_t s_cost[kTries];
+  __shared__ int s_per[kTries];
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  int n_seg = 0, n_valid = 0;
-  int64_t total;
+  Kept y;
+  {
+    int32_t* p = a.batch <= kHere ? s_kept : a.kept;
+    const int n = a.batch <= kHere ? kHere + 1 : a.batch + 1;
+    y = Kept{p, p + n, p + 2 * n, p + 3 * n, p + 4 * n, p + 5 * n, p + 6 * n,
+             p + 7 * n, p + 8 * n, p + 9 * n, p + 10 * n, p + 11 * n};
+  }
+  int n_seg = 0, n_valid = 0, b0 = -1;
   if (a.shared) {
     n_seg = min(max(a.meta[0], 0), a.cap);
     n_valid = min(max(a.meta[1], 0), a.batch);
-    for (int i = tid; i <= a.batch; i += kNT) a.u_len[i] = 0, a.seg_part[i] = 0;
+    if (tid < a.batch) b0 = a.perm[tid];
+  }
+  for (int b = tid; b < a.batch; b += kNT) {
+    const int q0 = a.q_start[b], q1 = a.q_start[b + 1], kv = a.kv_len[b];
+    int n = 0;
+    if (q0 >= 0 && q0 < q1 && q1 <= a.T && a.req[q0] == b) n = q1 - q0;
+    y.n[b] = n > a.max_q || kv < n || kv > a.max_keys ? 0 : n;
+    y.q0[b] = q0;
+    y.kv[b] = kv;
+    y.u[b] = 0;
+  }
+  if (a.shared) {
+    for (int i = tid; i <= n_seg; i += kNT) {
+      const int g = i < n_seg ? a.seg_id[i] : -1;
+      y.begin[i] = min(max(a.seg_ptr[i], 0), n_valid);
+      // the whole pages of the prefix
+      int64_t u = 0;
+      if (g >= 0 && g < a.n_groups) u = min((int64_t)a.prefix_len[g], a.max_keys);
+      y.pre[i] = u <= 0 ? 0 : (int)(u & -(int64_t)a.page_size);
+      y.part[i] = 0;
+      y.req[i] = INT32_MAX;
+    }
     __syncthreads();
     // who could share
     for (int p = tid; p < n_valid; p += kNT) {
-      const int b = a.perm[p];
-      if (b < 0 || b >= a.batch) continue;
+      const int b = p == tid ? b0 : a.perm[p];
+      if (b < 0 || b >= a.batch || n_seg == 0) continue;
       int s = 0, z = n_seg;                              // the segment that holds p
       while (z - s > 1) {
         const int mid = (s + z) >> 1;
-        if (a.seg_ptr[mid] <= p) s = mid;
+        if (y.begin[mid] <= p) s = mid;
         else z = mid;
       }
-      int q0, kv;
-      const int n = tokens(a, b, q0, kv), u = n_seg > 0 ? prefix(a, s) : 0;
-      a.seg_of[b] = s;
-      if (n > 0 && u > 0 && (int64_t)n * a.r <= PLORA_ATTN_SHARE_ROWS && kv - n >= u) {
-        a.u_len[b] = u;
-        atomicAdd(&a.seg_part[s], 1);
+      const int n = y.n[b], u = y.pre[s];
+      y.seg[b] = s;
+      if (n > 0 && u > 0 && (int64_t)n * a.r <= PLORA_ATTN_SHARE_ROWS && y.kv[b] - n >= u) {
+        y.u[b] = u;
+        atomicAdd(&y.part[s], 1);
+        atomicMin(&y.req[s], b);
       }
     }
     __syncthreads();
     // members: not alone in their group; their tokens in group order
-    int64_t carry = 0;
+    uint32_t carry[1] = {0};
     for (int p0 = 0; p0 < n_valid; p0 += kNT) {
       const int p = p0 + tid;
-      int b = p < n_valid ? a.perm[p] : -1, q0 = 0, kv, n = 0;
+      int b = p >= n_valid ? -1 : p == tid ? b0 : a.perm[p], n = 0;
       if (b < 0 || b >= a.batch) b = -1;
-      if (b >= 0 && a.u_len[b] > 0) {
-        if (a.seg_part[a.seg_of[b]] >= 2) n = tokens(a, b, q0, kv);
-        else a.u_len[b] = 0;
+      if (b >= 0 && y.u[b] > 0) {
+        if (y.part[y.seg[b]] >= 2) n = y.n[b];
+        else y.u[b] = 0;
       }
-      const int64_t at = carry + scan(n, red, total);
-      carry += total;
-      if (p < n_valid) a.moff[p] = (int)at;
+      uint32_t at[1] = {(uint32_t)n};
+      scan(at, carry, red1);
+      if (p < n_valid) y.moff[p] = at[0];
       if (n > 0) {
-        a.place[b] = (int)at;
-        for (int j = 0; j < n; ++j)
-          if (at + j < a.T) a.order[at + j] = q0 + j;
+        y.place[b] = at[0];
+        for (int j = 0; j < n && (int)at[0] + j < a.T; ++j) a.order[at[0] + j] = y.q0[b] + j;
       }
     }
-    if (tid == 0) a.moff[n_valid] = (int)carry;
-    __syncthreads();
+    if (tid == 0) y.moff[n_valid] = carry[0];
   }
-  // a set's rows and keys: the groups' prefixes, then the requests' own
+  __syncthreads();
+  // the sets: the groups' prefixes, then the requests' own keys
+  const int n_sets = n_seg + a.batch;
+  const auto members = [&](int s, int& tok) {            // a group's tokens
+    tok = y.moff[y.begin[s]];
+    return y.moff[y.begin[s + 1]] - tok;
+  };
   const auto set_of = [&](int i, int& rows, int& keys) {
     int64_t n;
+    int tok;
     if (i < n_seg) {
-      n = a.moff[seg_begin(a, i + 1, n_valid)] - a.moff[seg_begin(a, i, n_valid)];
-      keys = prefix(a, i);
+      n = members(i, tok);
+      keys = y.pre[i];
     } else {
-      int q0, kv;
-      n = tokens(a, i - n_seg, q0, kv);
-      keys = kv - (a.shared ? a.u_len[i - n_seg] : 0);
+      n = y.n[i - n_seg];
+      keys = y.kv[i - n_seg] - y.u[i - n_seg];
     }
     n *= a.r;
     rows = n > 0 && n <= INT32_MAX && keys > 0 ? (int)n : 0;
   };
-  const int n_sets = n_seg + a.batch;
   // work of each kind, in tiles x keys
-  int64_t few_work = 0, tile_work = 0;
+  double few_work = 0, tile_work = 0;
   for (int i = tid; i < n_sets; i += kNT) {
     int rows, keys;
     set_of(i, rows, keys);
-    if (rows == 0) continue;
-    if (rows > kFew) tile_work += (int64_t)((rows + kTile - 1) / kTile) * keys;
-    else few_work += keys;
+    if (rows > kFew) tile_work += (double)((rows + kTile - 1) / kTile) * keys;
+    else if (rows > 0) few_work += keys;
   }
-  int64_t all_few, all_tile;
-  scan(few_work, red, all_few);
-  scan(tile_work, red, all_tile);
-  const auto per_piece = [&](int64_t work, int target, int least, int step) {
-    const int64_t t = (target + a.kv_heads - 1) / a.kv_heads;
-    const int64_t c = max((work + t - 1) / t, (int64_t)least);
-    return (int)min((c + step - 1) / step * step, (int64_t)PLORA_PAGED_MAX_KEYS);
-  };
-  Rule rule;
-  rule.few_keys = per_piece(all_few, kFewTarget, kMinFew, kFewStep);
-  rule.tile_keys = PLORA_PAGED_MAX_KEYS;
-  if (all_tile > 0) {
-    int64_t items[kTries] = {};
-    int longest[kTries] = {}, per[kTries];
+  few_work = wave_scan(few_work, Add{});
+  tile_work = wave_scan(tile_work, Add{});
+  if (lane == 63) s_work[wv][0] = few_work, s_work[wv][1] = tile_work;
+  __syncthreads();
+  few_work = tile_work = 0;
 #pragma unroll
-    for (int k = 0; k < kTries; ++k) per[k] = per_piece(all_tile, kTry[k], kMinTile, kTileStep);
-    for (int i = tid; i < n_sets; i += kNT) {
-      int rows, keys;
-      set_of(i, rows, keys);
-      if (rows <= kFew) continue;
-#pragma unroll
-      for (int k = 0; k < kTries; ++k) {
-        const Cut c = cut(rows, keys, Rule{1, per[k]});
-        items[k] += (int64_t)c.tiles * c.pieces;
-        longest[k] = max(longest[k], c.keys);
+  for (int w = 0; w < kWaves; ++w) few_work += s_work[w][0], tile_work += s_work[w][1];
+  const int few_keys = per_piece(few_work, kFewTarget, a.kv_heads, kMinFew, kFewStep);
+  int tile_keys = PLORA_PAGED_MAX_KEYS;
+  if (tile_work > 0) {
+    const int per = per_piece(tile_work, kTry[wv], a.kv_heads, kMinTile, kTileStep);
+    int64_t items = 0;
+    int longest = 0;
+    for (int i0 = 0; i0 < n_sets; i0 += kNT) {
+      const int m = min(kNT, n_sets - i0);
+      int rows = 0, keys = 0;
+      if (tid < m) set_of(i0 + tid, rows, keys);
+      s_tiles[tid] = rows > kFew ? (rows + kTile - 1) / kTile : 0;
+      s_keys[tid] = keys;
+      __syncthreads();
+      for (int j = lane; j < m; j += 64) {
+        const int t = s_tiles[j];
+        if (t == 0) continue;
+        const Cut c = cut(kTile, s_keys[j], 1, per);
+        items += (int64_t)t * c.pieces;
+        longest = max(longest, c.keys);
       }
+      __syncthreads();
     }
-#pragma unroll
-    for (int k = 0; k < kTries; ++k) {
-      for (int d = 32; d; d >>= 1) {
-        items[k] += __shfl_xor(items[k], d, 64);
-        longest[k] = max(longest[k], __shfl_xor(longest[k], d, 64));
-      }
-      if (lane == 0) s_items[k][wv] = items[k], s_longest[k][wv] = longest[k];
+    items = wave_scan(items, Add{});
+    longest = wave_scan(longest, Max{});
+    if (lane == 63) {
+      s_cost[wv] = (items * a.kv_heads + kTileSlots - 1) / kTileSlots * (longest + kTileStart);
+      s_per[wv] = per;
     }
     __syncthreads();
-    if (tid == 0) {
-      int64_t least = INT64_MAX;
+    int64_t least = INT64_MAX;
 #pragma unroll
-      for (int k = 0; k < kTries; ++k) {
-        int64_t n = 0;
-        int len = 0;
-        for (int w = 0; w < kWaves; ++w) n += s_items[k][w], len = max(len, s_longest[k][w]);
-        const int64_t cost = (n * a.kv_heads + kTileSlots - 1) / kTileSlots * (len + kTileStart);
-        if (cost < least) least = cost, rule.tile_keys = per[k];
-      }
-    }
+    for (int k = 0; k < kTries; ++k)
+      if (s_cost[k] < least) least = s_cost[k], tile_keys = s_per[k];
   }
-  if (tid == 0) s_rule = rule;
-  __syncthreads();
-  rule = s_rule;
-  // items: the groups' prefixes first, then the requests' own keys
-  int64_t few_n = 0, tile_n = 0, part_n = 0;
-  for (int pass = a.shared ? 0 : 1; pass < 2; ++pass) {
-    const int count = pass == 0 ? n_seg : a.batch;
-    for (int i0 = 0; i0 < count; i0 += kNT) {
-      const int i = i0 + tid, m = min(kNT, count - i0);
-      Set x{};
-      x.req = -1;
-      int64_t rows = 0;
-      int u = 0;
-      if (i < count && pass == 0) {
-        const int p0 = seg_begin(a, i, n_valid), p1 = seg_begin(a, i + 1, n_valid);
-        x.tok = a.moff[p0];
-        rows = (int64_t)(a.moff[p1] - x.tok) * a.r;
-        x.hi = prefix(a, i);
-        x.gathered = 1;
-        if (rows > 0) x.req = a.req[a.order[min(x.tok, a.T - 1)]];
-      } else if (i < count) {
-        int q0, kv;
-        const int n = tokens(a, i, q0, kv);
-        u = a.shared ? a.u_len[i] : 0;
-        rows = (int64_t)n * a.r;
-        x.tok = q0;
-        x.req = i;
-        x.lo = u;
-        x.hi = kv;
-      }
-      if (rows <= 0 || rows > INT32_MAX || x.hi <= x.lo) rows = 0;
-      x.rows = (int)rows;
-      int64_t items = 0, part = 0;
-      if (rows > 0) {
-        x.c = cut(x.rows, x.hi - x.lo, rule);
-        items = (int64_t)x.c.tiles * x.c.pieces;
-        part = pass == 0 || u > 0 || x.c.pieces > 1 ? rows * x.c.pieces : 0;
-      }
-      int64_t few_total, tile_total, part_total;
-      const int64_t fb = few_n + scan(x.c.few ? items : 0, red, few_total);
-      const int64_t tb = tile_n + scan(x.c.few ? 0 : items, red, tile_total);
-      const int64_t pb = part_n + scan(part, red, part_total);
-      x.base = x.c.few ? fb : tb;
-      // (never past the caps for lengths that agree with the shape)
-      const int64_t cap = x.c.few ? a.few_cap : a.tile_cap;
-      if (x.base + items > cap || pb + part > a.part_cap) x.rows = 0;
-      x.part = part > 0 ? (int)pb : -1;
-      if (i < count && pass == 0) a.seg_part[i] = x.rows > 0 ? x.part : -1;
-      if (i < count && pass == 1) {
-        ReqInfo f{};
-        f.part = x.part;
-        f.splits = x.c.pieces;
-        f.rows = x.rows;
-        f.pre_part = -1;
-        f.state = x.rows == 0 ? 0 : x.part < 0 ? 2 : 1;
-        if (u > 0 && x.rows > 0) {
-          const int s = a.seg_of[i], t0 = a.moff[seg_begin(a, s, n_valid)];
-          const int all = (a.moff[seg_begin(a, s + 1, n_valid)] - t0) * a.r;
-          f.pre_part = a.seg_part[s];
-          f.pre_rows = all;
-          f.pre_splits = cut(all, u, rule).pieces;
-          f.pre_row = (a.place[i] - t0) * a.r;
-          if (f.pre_part < 0) f.state = 0;
-        }
-        a.info[i] = f;
-      }
-      sets[tid] = x;
-      __syncthreads();
-      for (int k = wv; k < m; k += kWaves) {
-        const Set& y = sets[k];
-        Item* list = y.c.few ? a.few : a.tile;
-        const int64_t cap = y.c.few ? a.few_cap : a.tile_cap;
-        const int64_t items = min((int64_t)y.c.tiles * y.c.pieces, cap - y.base);
-        for (int j = lane; j < items; j += 64) {
-          // the last rows, which see the most keys, first
-          const int tile = y.c.tiles - 1 - j / y.c.pieces, piece = j % y.c.pieces;
-          Item it;
-          it.tok = y.tok;
-          it.row = tile * kTile;
-          it.rows = min(y.rows - it.row, kTile);      // none if the set did not fit
-          it.req = y.req;
-          it.lo = y.lo + piece * y.c.keys;
-          it.hi = min(y.hi, it.lo + y.c.keys);
-          it.part = y.part < 0 ? -1 : y.part + piece * y.rows + it.row;
-          it.gathered = y.gathered;
-          list[y.base + j] = it;
-        }
-      }
-      __syncthreads();
-      few_n += few_total;
-      tile_n += tile_total;
-      part_n += part_total;
+  // items
+  uint32_t sum[3] = {0, 0, 0};                           // few, tiles, rows of partials
+  for (int i0 = 0; i0 < n_sets; i0 += kNT) {
+    const int i = i0 + tid, b = i - n_seg;
+    const bool own = i < n_sets && b >= 0;
+    Set x{};
+    x.req = -1;
+    int u = 0, rows, keys;
+    if (tid == 0) s_bigs = 0;
+    if (i < n_sets) {
+      set_of(i, rows, keys);
+      x.rows = rows;
     }
+    if (own) {
+      u = y.u[b];
+      x.tok = y.q0[b];
+      x.req = b;
+      x.lo = u;
+      x.hi = y.kv[b];
+    } else if (i < n_sets) {
+      members(i, x.tok);
+      x.hi = y.pre[i];
+      x.gathered = 1;
+      x.req = y.req[i];
+    }
+    int64_t items = 0, part = 0;
+    if (x.rows > 0) {
+      x.c = cut(x.rows, x.hi - x.lo, few_keys, tile_keys);
+      items = (int64_t)x.c.tiles * x.c.pieces;
+      if (!own || u > 0 || x.c.pieces > 1) part = (int64_t)x.rows * x.c.pieces;
+    }
+    uint32_t at[3] = {(uint32_t)min(x.c.few ? items : 0, (int64_t)kMany),
+                      (uint32_t)min(x.c.few ? 0 : items, (int64_t)kMany),
+                      (uint32_t)min(part, (int64_t)kMany)};
+    scan(at, sum, red3);
+    x.base = x.c.few ? at[0] : at[1];
+    x.part = part > 0 ? (int)at[2] : -1;
+    // (never past the caps for lengths that agree with the shape)
+    const int cap = x.c.few ? a.few_cap : a.tile_cap;
+    if (x.base + items > cap || at[2] + part > a.part_cap) x.rows = 0;
+    x.items = (int)min(items, (int64_t)max(cap - x.base, 0));
+    if (i < n_seg) {
+      y.part[i] = x.rows > 0 ? x.part : -1;
+      y.splits[i] = x.c.pieces;
+    }
+    if (x.items > kOwn) {
+      s_sets[tid] = x;
+      s_big[atomicAdd(&s_bigs, 1)] = tid;
+    } else {
+      int tile = x.c.tiles - 1, piece = 0;
+      for (int j = 0; j < x.items; ++j) {
+        emit(a, x, j, tile, piece);
+        if (++piece == x.c.pieces) piece = 0, --tile;
+      }
+    }
+    __syncthreads();
+    if (own) {
+      ReqInfo f{};
+      f.part = x.part;
+      f.splits = x.c.pieces;
+      f.rows = x.rows;
+      f.pre_part = -1;
+      f.state = x.rows == 0 ? 0 : x.part < 0 ? 2 : 1;
+      if (u > 0 && x.rows > 0) {
+        const int s = y.seg[b];
+        int tok;
+        f.pre_rows = members(s, tok) * a.r;
+        f.pre_part = y.part[s];
+        f.pre_splits = y.splits[s];
+        f.pre_row = (y.place[b] - tok) * a.r;
+        if (f.pre_part < 0) f.state = 0;
+      }
+      a.info[b] = f;
+    }
+    const int bigs = s_bigs;
+    for (int k = wv; k < bigs; k += kWaves) {
+      const Set& z = s_sets[s_big[k]];
+      // the last rows, which see the most keys, first
+      for (int j = lane; j < z.items; j += 64)
+        emit(a, z, j, z.c.tiles - 1 - j / z.c.pieces, j % z.c.pieces);
+    }
+    __syncthreads();
   }
   if (tid == 0) {
     PlanHeader h{};
-    h.few = (int)min(few_n, (int64_t)a.few_cap);
-    h.tiles = (int)min(tile_n, (int64_t)a.tile_cap);
-    h.part_rows = (int)min(part_n, a.part_cap);
-    h.few_keys = rule.few_keys;
-    h.tile_keys = rule.tile_keys;
+    h.few = min((int)sum[0], a.few_cap);
+    h.tiles = min((int)sum[1], a.tile_cap);
+    h.part_rows = min((int)sum[2], a.part_cap);
+    h.few_keys = few_keys;
+    h.tile_keys = tile_keys;
     // rounded up: all tiles have come by the last work group, at most one an eight
     const uint64_t few8 = ((uint64_t)h.few * a.kv_heads + 7) / 8;
     const uint64_t tile8 = ((uint64_t)h.tiles * a.kv_heads + 7) / 8;
@@ -406,7 +479,8 @@ extern "C" plora_status plora_attn_plan(const plora_kv_step* step, const plora_a
   a.info = reinterpret_cast<ReqInfo*>(base + l.req);
   a.few_cap = b.few_cap;
   a.tile_cap = b.tile_cap;
-  a.part_cap = b.part_rows;
+  a.part_cap = (int32_t)b.part_rows;
+  a.kept = reinterpret_cast<int32_t*>(base + l.kept);
   if (seg && n_groups > 0) {
     a.shared = 1;
     a.n_groups = n_groups;
@@ -416,13 +490,6 @@ extern "C" plora_status plora_attn_plan(const plora_kv_step* step, const plora_a
     a.seg_id = seg->seg_id;
     a.meta = seg->meta;
     a.prefix_len = prefix_len;
-    int32_t* s = reinterpret_cast<int32_t*>(base + l.scratch);
-    const int32_t n = shape->batch + 1;
-    a.u_len = s;
-    a.place = s + n;
-    a.seg_of = s + 2 * n;
-    a.moff = s + 3 * n;
-    a.seg_part = s + 4 * n;
   }
   clear_error();
   hipLaunchKernelGGL(attn_plan_kernel, dim3(1), dim3(kNT), 0, stream, a);

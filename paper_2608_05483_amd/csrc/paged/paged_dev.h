@@ -11,6 +11,7 @@
 
 namespace paged {
 
+typedef int32_t i32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -58,7 +59,7 @@ struct Fp16 {
 
 inline bool aligned(const void* p, size_t n) { return (reinterpret_cast<uintptr_t>(p) % n) == 0; }
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
-inline bool pow2(int32_t v) { return v > 0 && (v & (v - 1)) == 0; }
+constexpr bool pow2(int32_t v) { return v > 0 && (v & (v - 1)) == 0; }
 inline bool page_size_ok(int32_t s) {
   return pow2(s) && s >= PLORA_PAGE_MIN && s <= PLORA_PAGE_MAX;
 }

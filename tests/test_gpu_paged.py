@@ -367,6 +367,20 @@ def test_shared_prefixes(G, P, dt, D, H, KH, hi):
     check(b.run(0.1), *b.ref(0.1), dt, 1200)
 
 
+@pytest.mark.parametrize("share", [False, True])
+def test_many_requests(G, P, share):
+    """More requests than the plan's kernel keeps in LDS, and more than it takes at a
+    time; 70 groups and some requests in none."""
+    rng = np.random.default_rng(5)
+    n, prefix = 1300, rng.integers(0, 80, 70)
+    group = rng.integers(-1, 70, n)
+    past = rng.integers(0, 100, n) + np.where(group >= 0, prefix[group], 0)
+    new = np.where(rng.random(n) < 0.02, 20, rng.integers(0, 3, n))
+    b = Batch(G, P, past, new, 2, 1, 64, group=group if share else None,
+              prefix=prefix if share else (), seed=5)
+    check(b.run(0.125), *b.ref(0.125), BF, 200)
+
+
 def test_a_request_inside_its_prefix_does_not_share(G, P):
     """A request that is still writing the prefix attends alone; ids outside the
     groups and negative prefixes share nothing."""

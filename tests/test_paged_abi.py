@@ -175,6 +175,12 @@ def test_attn_paged_refusals(kw, want):
     assert attn_status(**kw) == want
 
 
+def test_a_launch_of_too_many_threads_is_refused():
+    big = dict(batch=1, T=1 << 20)
+    assert attn_status(s=step(**big), sh=shape(heads=65536, kv_heads=1024, max_q=1 << 20, **big),
+                       c=cache(kv_heads=1024)) == UNS
+
+
 def test_sizes():
     assert G.attn_plan_bytes(shape(batch=0)) == 0 and G.attn_plan_bytes(shape(T=0)) == 0
     assert G.attn_plan_bytes(shape(heads=7)) == 0
