@@ -28,7 +28,7 @@ struct AttnArgs {
   int32_t key_stride, n_pages, log_page, max_pages;
   const int32_t *table, *pos, *order, *req, *q_start;
   const PlanHeader* head;
-  const Item *few, *tile;
+  const Item *few, *last_few, *tile;
   const ReqInfo* info;
   int32_t batch, T, r, kv_heads;
   float c;                  // |scale| log2(e)
@@ -406,9 +406,9 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
   __shared__ f32x4 o01[2 * kFew * D / 4], o23[2 * kFew * D / 4];
   __shared__ FewShared sh;
   // (the grid covers the items' cap, so the item may be read beside their number)
-  const int item = blockIdx.x / a.kv_heads;
-  const Item it = a.few[item];
-  if (item >= a.head->few) return;
+  const int item = blockIdx.x / a.kv_heads, first = a.head->few;
+  if (item >= first + a.head->later) return;
+  const Item it = item < first ? a.few[item] : a.last_few[first - item];
   few_item<Ty, D, POL, false>(a, it, blockIdx.x % a.kv_heads, sh, o01, o23);
 }
 
@@ -679,12 +679,16 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
   }
 }
 
-// Both kinds of items in one launch, in turn in proportion to their numbers, so that
-// the compute units hold work groups of both at once: the one kind is bound by
-// reading, the other by the matrix units (256 requests in 6 groups, 176 us in two
-// launches, 165 so).  Eight work groups in a row are of one kind, so that a head's
-// items, which share K and V, stay on one XCD where the key heads are a multiple
-// of 8.
+// Both kinds of items in one launch, the one bound by reading, the other by the
+// matrix units.  They come in turn, kRun eights of each until one kind is used up:
+// a run is a work group for every compute unit, and each holds two, so that a tile
+// item has one of another kind beside it, and the long tile items have begun early.
+// Both calls of a layer, 256 requests in 6 groups: 163 us; in turn by each eight 176,
+// spread in proportion over the launch 193, all tile items first 163 (45 requests in
+// 3 groups x 40 heads: 93, 96, 99, 102).  Eight work groups in a row are of one kind,
+// so that a head's items, which share K and V, stay on one XCD where the key heads
+// are a multiple of 8.
+constexpr uint32_t kRun = 32;
 template <class Ty, int D, int POL>
 __global__ __launch_bounds__(kNT, 2) void items_kernel(AttnArgs a) {
   // (buffers by name: reads of one are seen not to meet the loads into the other)
@@ -693,14 +697,21 @@ __global__ __launch_bounds__(kNT, 2) void items_kernel(AttnArgs a) {
   __shared__ FewShared sh;
   static_assert(sizeof(s_k0) == 2 * kFew * D * sizeof(float), "two wavefronts' outputs");
   const uint32_t turn = blockIdx.x >> 3, in = blockIdx.x & 7;
-  const uint64_t rate = a.head->tile_rate;
-  const uint32_t t0 = (uint32_t)(turn * rate >> 32), t1 = (uint32_t)((turn + 1) * rate >> 32);
-  const bool tile = t1 > t0;
-  const uint32_t index = (tile ? t0 : turn - t0) * 8 + in, item = index / a.kv_heads;
+  const int few = a.head->few, all_few = few + a.head->later;
+  const uint32_t tiles = ((uint32_t)a.head->tiles * a.kv_heads + 7) / 8;
+  const uint32_t fews = ((uint32_t)all_few * a.kv_heads + 7) / 8;
+  // (of each kind before this one, while both last)
+  const uint32_t t0 = turn / (2 * kRun) * kRun + min(turn % (2 * kRun), kRun), f0 = turn - t0;
+  bool tile = turn % (2 * kRun) < kRun;
+  if (f0 > fews || (f0 == fews && !tile)) tile = true;
+  else if (t0 > tiles || (t0 == tiles && tile)) tile = false;
+  const uint32_t index =
+      (tile ? turn - min(f0, fews) : turn - min(t0, tiles)) * 8 + in, item = index / a.kv_heads;
   const int kvh = index % a.kv_heads;
   // (the work groups behind the last item would pass the lists' ends)
-  if (item >= (uint32_t)(tile ? a.head->tiles : a.head->few)) return;
-  const Item it = (tile ? a.tile : a.few)[item];
+  if (item >= (uint32_t)(tile ? a.head->tiles : all_few)) return;
+  const Item it = tile ? a.tile[item]
+                       : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
   if (tile)
     tile_item<Ty, D>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
   else
@@ -936,6 +947,7 @@ extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t
   a.q_start = step->q_start;
   a.head = reinterpret_cast<const PlanHeader*>(p);
   a.few = reinterpret_cast<const Item*>(p + l.few);
+  a.last_few = a.few + b.few_cap - 1;
   a.tile = reinterpret_cast<const Item*>(p + l.tile);
   a.order = reinterpret_cast<const int32_t*>(p + l.order);
   a.info = reinterpret_cast<const ReqInfo*>(p + l.req);

@@ -95,11 +95,10 @@ inline PlanLayout plan_layout(const plora_attn_shape& s, const Bounds& b) {
   return l;
 }
 struct PlanHeader {
-  int32_t few, tiles;          // items
+  int32_t few, tiles;          // items: of few rows, from their list's start; of more
   int32_t part_rows;
   int32_t few_keys, tile_keys; // keys per piece
-  int32_t reserved;
-  uint64_t tile_rate;          // eights of tile work groups among all, times 2^32
+  int32_t later;               // short items of few rows, from their list's end
 };
 
 inline bool shape_ok(const plora_attn_shape& s) {

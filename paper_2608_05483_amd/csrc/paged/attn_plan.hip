@@ -154,17 +154,20 @@ __device__ __forceinline__ void emit(const PlanArgs& a, const Set& x, int j, int
 // ones cost little (64 requests x 32 heads x 512..4096 keys: 402 us at 768, 392 at
 // 2048, 380 at 4096), and pieces of less than 512 keys pay more for their start and
 // their partials than they gain (one request of 30011 keys on 8 heads, both
-// kernels: 42 us at 256, 33 at 512).
+// kernels: 42 us at 256, 33 at 512).  Sets of at most half of that come last, so that
+// what is begun last is short (256 requests of 33..543 keys on 8 heads: 67 us in the
+// requests' order, 63 so; 180 of 9..708 on 40: 230 and 223).
 // Tile items: the number of pieces changes how many rounds the chip's kTileSlots
 // work groups (two per compute unit) take, so several cuts are tried, a wavefront
 // each, and the one whose rounds x (longest piece + kTileStart) is least is taken
 // (256 requests in 6 groups x 64 heads over 8, prefixes of 4000 keys: 608 work
-// groups, two rounds, 81 us; 456, one, 64; the tile items alone).
+// groups, two rounds, 81 us; 456, one, 64; the tile items alone).  kTileStart is what
+// a piece costs beside its keys, most of it the writing and reading of its partials.
 //
 // Once a step and bound by latency: dependent loads, barriers, and code that is
 // fetched for the first time.
 constexpr int kMinFew = 512, kMinTile = 256;
-constexpr int kTileSlots = 512, kTileStart = 128;
+constexpr int kTileSlots = 512, kTileStart = 512;
 constexpr int kTries = kWaves;
 __constant__ const int kTry[kTries] = {256, 320, 384, 448, 512, 640, 768, 1024};
 static_assert(kTileTarget == 1024, "the finest cut tried bounds the items");
@@ -184,7 +187,7 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
   __shared__ int32_t s_kept[kKeptArrays * (kHere + 1)];
   __shared__ Set s_sets[kNT];
   __shared__ int s_keys[kNT], s_tiles[kNT], s_big[kNT], s_bigs;
-  __shared__ uint32_t red1[kWaves][1], red3[kWaves][3];
+  __shared__ uint32_t red1[kWaves][1], red4[kWaves][4];
   __shared__ double s_work[kWaves][2];
   __shared__ int64_t s_cost[kTries];
   __shared__ int s_per[kTries];
@@ -332,7 +335,7 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
       if (s_cost[k] < least) least = s_cost[k], tile_keys = s_per[k];
   }
   // items
-  uint32_t sum[3] = {0, 0, 0};                           // few, tiles, rows of partials
+  uint32_t sum[4] = {0, 0, 0, 0};                        // few, tiles, rows of partials, later
   for (int i0 = 0; i0 < n_sets; i0 += kNT) {
     const int i = i0 + tid, b = i - n_seg;
     const bool own = i < n_sets && b >= 0;
@@ -362,16 +365,17 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
       items = (int64_t)x.c.tiles * x.c.pieces;
       if (!own || u > 0 || x.c.pieces > 1) part = (int64_t)x.rows * x.c.pieces;
     }
-    uint32_t at[3] = {(uint32_t)min(x.c.few ? items : 0, (int64_t)kMany),
+    const bool later = x.rows > 0 && x.c.few && x.c.pieces == 1 && x.c.keys <= few_keys / 2;
+    uint32_t at[4] = {(uint32_t)min(x.c.few && !later ? items : 0, (int64_t)kMany),
                       (uint32_t)min(x.c.few ? 0 : items, (int64_t)kMany),
-                      (uint32_t)min(part, (int64_t)kMany)};
-    scan(at, sum, red3);
-    x.base = x.c.few ? at[0] : at[1];
+                      (uint32_t)min(part, (int64_t)kMany), later};
+    scan(at, sum, red4);
+    x.base = later ? a.few_cap - 1 - (int)at[3] : x.c.few ? at[0] : at[1];
     x.part = part > 0 ? (int)at[2] : -1;
     // (never past the caps for lengths that agree with the shape)
     const int cap = x.c.few ? a.few_cap : a.tile_cap;
-    if (x.base + items > cap || at[2] + part > a.part_cap) x.rows = 0;
-    x.items = (int)min(items, (int64_t)max(cap - x.base, 0));
+    if (x.base < 0 || x.base + items > cap || at[2] + part > a.part_cap) x.rows = 0;
+    x.items = x.base < 0 ? 0 : (int)min(items, (int64_t)max(cap - x.base, 0));
     if (i < n_seg) {
       y.part[i] = x.rows > 0 ? x.part : -1;
       y.splits[i] = x.c.pieces;
@@ -417,14 +421,11 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
   if (tid == 0) {
     PlanHeader h{};
     h.few = min((int)sum[0], a.few_cap);
+    h.later = min((int)sum[3], a.few_cap - h.few);
     h.tiles = min((int)sum[1], a.tile_cap);
     h.part_rows = min((int)sum[2], a.part_cap);
     h.few_keys = few_keys;
     h.tile_keys = tile_keys;
-    // rounded up: all tiles have come by the last work group, at most one an eight
-    const uint64_t few8 = ((uint64_t)h.few * a.kv_heads + 7) / 8;
-    const uint64_t tile8 = ((uint64_t)h.tiles * a.kv_heads + 7) / 8;
-    h.tile_rate = tile8 ? ((tile8 << 32) + few8 + tile8 - 1) / (few8 + tile8) : 0;
     *a.head = h;
   }
 }
