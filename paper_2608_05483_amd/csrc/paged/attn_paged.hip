@@ -307,10 +307,11 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
     for (int i = 0; i < 8; ++i) mx = fmaxf(mx, t[i]);
     mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
     mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
-    const float ms = mx == -INFINITY ? 0.f : mx;
+    float ms = mx == -INFINITY ? 0.f : mx;
     const float al = exp2_(m - ms);
     m = mx;
     l *= al;
+    ms -= Ty::kLift;
     u32x4 ph, pl;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -391,7 +392,7 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
                         any ? 1.f / L : 0.f);
     } else {
       const int64_t at = ((int64_t)it.part + i) * a.kv_heads + kvh;
-      if (e == 0) a.pm[at] = M, a.pl[at] = L;
+      if (e == 0) a.pm[at] = M - Ty::kLift, a.pl[at] = L;
       store_part<kV>(a.po + at * D + e, o);
     }
   }
@@ -421,9 +422,9 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
 // 16 dimensions of four keys and each gets one dimension's four).
 // The weights are formed against the row's present maximum before it is known
 // whether that still stands: it is only raised, the output rescaled and the weights
-// formed again, if a lane's sum of 32 passes 2^13.  So no maximum is looked for in
-// most steps; no weight passes 2^13 then, which either type holds with its full
-// precision.  The weights are summed as rounded to the type, which they are for the
+// formed again, if a lane's sum of 32 passes kBar (bf16 2^13; fp16 2^16, above which
+// a weight becomes infinite and the sum with it).  So no maximum is looked for in
+// most steps, and no weight is more than its type holds.  The weights are summed as rounded to the type, which they are for the
 // product with V: its rounding errors average out below the output's own, and a
 // second product for the rest would add half to the work that bounds the kernel.
 // Bound by the matrix units and what they cannot hide: for 64 keys and 32 rows 32
@@ -434,8 +435,6 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
 // through registers into LDS and V transposed there 2.4 us; with a maximum each step
 // and a sum by additions 2.7; eight wavefronts a work group in two phases, one
 // side's products beside the other's exponentials, 2.8.
-constexpr float kBar = 8192.f;
-
 // Schedules n products, each fed by r reads from LDS, four products' reads ahead.
 template <int N, int R>
 __device__ __forceinline__ void feed() {
@@ -591,7 +590,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
       }
       u32x4 p[4];
       const auto weights = [&]() {
-        const float ms = m == -INFINITY ? 0.f : m;
+        const float ms = (m == -INFINITY ? 0.f : m) - Ty::kTileLift;
         float sum0 = 0.f, sum1 = 0.f;
 #pragma unroll
         for (int b = 0; b < 2; ++b)
@@ -616,7 +615,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
         const float ms = mx == -INFINITY ? 0.f : mx;
         const float al = exp2_(m - ms);
         m = mx;
-        bar = m == -INFINITY ? first : kBar;
+        bar = m == -INFINITY ? first : Ty::kBar;
         l *= al;
 #pragma unroll
         for (int d = 0; d < kV; ++d)
@@ -657,7 +656,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
   if (mine) {
     const float inv = any ? 1.f / l : 0.f;
     const int64_t at = ((int64_t)it.part + 32 * wv + n) * a.kv_heads + kvh;
-    if (it.part >= 0 && h == 0) a.pm[at] = m, a.pl[at] = l;
+    if (it.part >= 0 && h == 0) a.pm[at] = m - Ty::kTileLift, a.pl[at] = l;
 #pragma unroll
     for (int d = 0; d < kV; ++d)
 #pragma unroll

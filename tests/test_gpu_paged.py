@@ -299,6 +299,30 @@ def check(got, ref, size, dt, keys, vmax=6.0):
     assert worst <= 0, worst
 
 
+@pytest.mark.parametrize("D", [128, 64])
+@pytest.mark.parametrize("new", [1, 40])
+def test_many_keys_of_little_weight_fp16(G, P, D, new):
+    """Every 64th key has the weight 1 and a value of zero; what is left of the
+    output is that of the others, whose weights of 2^-25.5 are below half of fp16's
+    smallest number.  A weight may be off by half of that 2^8 lower (2^-33)."""
+    b = Batch(G, P, [700], [new], 2, 1, D, page=32, dt=HF)
+    scale = 1.0 / 16
+    b.q.fill_(1.0)
+    sink = 25.5 * math.log(2.0) / (D * scale)
+    table = b.step.table.cpu().numpy()[0]
+    off = torch.arange(32, device="cuda")
+    for j in range(-(-(700 + new) // 32)):
+        first = ((j * 32 + off) % 64 == 0)[None, :, None]
+        k, v = b.cache.k[int(table[j])], b.cache.v[int(table[j])]
+        k.copy_(torch.where(first, sink, 0.0).expand_as(k))
+        v.copy_(torch.where(first, 0.0, 30000.0).expand_as(v))
+    got = b.run(scale)
+    ref, size = b.ref(scale)
+    assert ref.min() > 0.02
+    tol = half_step(HF) * np.abs(ref) + (half_step(HF) + 1e-4) * size + 64 * 2.0 ** -33 * 30000
+    assert (np.abs(got - ref) <= tol).all()
+
+
 @pytest.mark.parametrize("dt,D", [(BF, 128), (HF, 128), (BF, 64), (HF, 64)])
 @pytest.mark.parametrize("H,KH", [(4, 4), (8, 1), (16, 1), (6, 2), (20, 1), (40, 2)])
 def test_decode(G, P, dt, D, H, KH):
