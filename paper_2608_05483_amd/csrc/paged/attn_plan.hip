@@ -39,35 +39,8 @@ struct Kept {
 };
 static_assert(sizeof(Kept) == kKeptArrays * sizeof(int32_t*), "");
 
-// A value moved over lanes, 0 where none comes (all lanes active).
-template <int CTRL, int ROWS, class V>
-__device__ __forceinline__ V moved(V x) {
-  if constexpr (sizeof(V) == 4) {
-    return __builtin_bit_cast(
-        V, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
-  } else {
-    const i32x2 w = __builtin_bit_cast(i32x2, x);
-    const i32x2 y = {__builtin_amdgcn_update_dpp(0, w[0], CTRL, ROWS, 0xf, false),
-                     __builtin_amdgcn_update_dpp(0, w[1], CTRL, ROWS, 0xf, false)};
-    return __builtin_bit_cast(V, y);
-  }
-}
-// Inclusive scan over a wavefront: within rows of 16 lanes, then over the rows.
-template <class V, class Op>
-__device__ __forceinline__ V wave_scan(V x, Op op) {
-  x = op(x, moved<0x111, 0xf>(x));
-  x = op(x, moved<0x112, 0xf>(x));
-  x = op(x, moved<0x114, 0xf>(x));
-  x = op(x, moved<0x118, 0xf>(x));
-  x = op(x, moved<0x142, 0xa>(x));
-  return op(x, moved<0x143, 0xc>(x));
-}
 // Counts, none below 0, are kept to 2^30, above every cap.
 constexpr uint32_t kMany = 1u << 30;
-struct Add {
-  template <class V>
-  __device__ V operator()(V a, V b) const { return a + b; }
-};
 struct AddCount {
   __device__ uint32_t operator()(uint32_t a, uint32_t b) const { return min(a + b, kMany); }
 };

@@ -14,34 +14,33 @@ constexpr int kChunk = kNT * kPer;      // requests scanned at a time
 constexpr int kTok = 512;               // tokens per work group
 constexpr int kWaves = kNT / 64;
 
-// Exclusive scan over the work group of one value a thread, in thread order,
-// with sums cut off at cap (min(a + b, cap) is associative for values >= 0);
-// total is the sum of all.  red holds kWaves words.
-__device__ __forceinline__ int block_scan(int x, int cap, int* red, int& total) {
+// Exclusive scans over the work group of N counts a thread, in thread order, without
+// a cut-off; total is the sums of all.
+template <int N>
+__device__ __forceinline__ void block_scan(uint32_t (&x)[N], uint32_t (&red)[kWaves][N],
+                                           uint32_t (&total)[N]) {
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
-  int inc = min(x, cap);
 #pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const int y = __shfl_up(inc, d, 64);
-    if (lane >= d) inc = min(inc + y, cap);
-  }
-  const int up = __shfl_up(inc, 1, 64);
-  int ex = lane ? up : 0;
-  if (lane == 63) red[wv] = inc;
-  __syncthreads();
-  int before = 0, all = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    if (w < wv) before = min(before + red[w], cap);
-    all = min(all + red[w], cap);
+  for (int i = 0; i < N; ++i) {
+    const uint32_t inc = wave_scan(x[i], Add{});
+    if (lane == 63) red[wv][i] = inc;
+    x[i] = inc - x[i];
   }
   __syncthreads();
-  total = all;
-  return min(before + ex, cap);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    total[i] = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wv) x[i] += red[w][i];
+      total[i] += red[w][i];
+    }
+  }
 }
 
-// Every work group scans all requests, a chunk of them at a time (two scans:
-// tokens, then pages of those that can be served), keeps the chunk's starts in
+// Every work group scans all requests, a chunk of them at a time (tokens, and the
+// pages of those that can be served: together where the tokens fit T, as then no
+// request is left out for them, else one after the other), keeps the chunk's starts in
 // LDS and writes those of its own kTok tokens that the chunk's requests hold: a
 // search by halves for the request, one or two loads for the page.  A new page
 // begins with a new token (page j of a request was not held, so j S >= past), and
@@ -58,7 +57,7 @@ __global__ __launch_bounds__(kNT) void kv_plan_kernel(
     int32_t* __restrict__ kv_len, int32_t* __restrict__ pos, int32_t* __restrict__ req,
     int64_t* __restrict__ slot, int32_t* __restrict__ meta) {
   __shared__ int s_start[kChunk], s_past[kChunk], s_off[kChunk];  // s_off -1: left out
-  __shared__ int red[kWaves];
+  __shared__ uint32_t red2[kWaves][2], red1[kWaves][1];
   const int tid = threadIdx.x, S1 = (1 << log_page) - 1;
   const int64_t most = (int64_t)max_pages << log_page;
   const int head = *free_head;
@@ -69,28 +68,38 @@ __global__ __launch_bounds__(kNT) void kv_plan_kernel(
   for (int c0 = 0; c0 < batch; c0 += kChunk) {
     const int m = min(kChunk, batch - c0);
     int p[kPer], n[kPer], need[kPer], st[kPer];
-    int sum = 0;
+    uint32_t x[2] = {0, 0}, total[2];
+    // (1024 counts of at most T + 1 do not overflow; the pages' sum may, and then is
+    // not used)
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int b = kPer * tid + i;
       p[i] = b < m ? past[c0 + b] : 0;
       n[i] = b < m ? n_new[c0 + b] : 0;
-      sum = min(sum + min(max(n[i], 0), T + 1), T + 1);
+      const bool ok = p[i] >= 0 && n[i] >= 0 && (int64_t)p[i] + n[i] <= most;
+      need[i] = ok ? ((p[i] + n[i] + S1) >> log_page) - ((p[i] + S1) >> log_page) : -1;
+      x[0] += min(max(n[i], 0), T + 1);
+      x[1] += max(need[i], 0);
     }
-    int total;
-    int at = min(block_scan(sum, T + 1, red, total) + tok_carry, T + 1);
-    int pages = 0;
+    block_scan(x, red2, total);
+    int at = min((int)x[0] + tok_carry, T + 1);
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       st[i] = at;
       at = min(at + min(max(n[i], 0), T + 1), T + 1);
-      const bool ok = p[i] >= 0 && n[i] >= 0 && (int64_t)p[i] + n[i] <= most && at <= T;
-      need[i] = ok ? ((p[i] + n[i] + S1) >> log_page) - ((p[i] + S1) >> log_page) : -1;
-      pages += max(need[i], 0);
+      if (at > T) need[i] = -1;
     }
-    tok_carry = min(tok_carry + total, T + 1);
-    int off = page_carry + block_scan(pages, INT32_MAX / 2, red, total);
-    page_carry += total;
+    tok_carry = min(tok_carry + (int)total[0], T + 1);
+    if (tok_carry > T) {
+      uint32_t y[1] = {0}, all[1];
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) y[0] += max(need[i], 0);
+      block_scan(y, red1, all);
+      x[1] = y[0];
+      total[1] = all[0];
+    }
+    int off = page_carry + (int)x[1];
+    page_carry += (int)total[1];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int b = kPer * tid + i;

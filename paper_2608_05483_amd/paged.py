@@ -117,7 +117,7 @@ def _heads(name: str, t, dtype: int):
 
 
 def _ints(name: str, t, dtype, n: int):
-    if t.dtype != dtype or t.numel() < n or not t.is_contiguous():
+    if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor of at least {n} entries expected")
     return t.data_ptr()
 
