@@ -11,19 +11,19 @@ namespace {
 constexpr int kNT = 256;
 constexpr int kBatch = 4;     // rows that a thread asks for before it uses any
 
-// One tensor of a launch: rows of (token, head).
+// One tensor of a launch: rows of (token, head).  The first is turned, with an out of
+// tokens; the others' outs are pools, addressed by slot (out_head within a page), the
+// second turned, the third copied.
 struct Part {
   const uint16_t* in;
   uint16_t* out;
-  int64_t in_token, in_head, out_token, out_head;   // (a pool: out_head within a page)
+  int64_t in_token, in_head, out_token, out_head;
   int32_t heads;
-  int32_t turned;           // else only copied
-  int32_t cached;           // out is a pool, addressed by slot
 };
 
 struct RopeArgs {
   Part part[3];
-  int32_t parts, rows;      // rows: heads of one token, all parts
+  int32_t rows;             // heads of one token, all parts
   int32_t rows_per;         // rows per work group
   int32_t units, rot_units; // units of a row, and how many of them turn
   int32_t log_lanes;        // lanes of a row, a power of two
@@ -76,6 +76,12 @@ __device__ __forceinline__ Words<W> pack(const float f[W]) {
   return u;
 }
 
+// One of three values (by value: the choice is then one of registers).
+template <class V>
+__device__ __forceinline__ V pick(bool third, bool second, V a, V b, V c) {
+  return third ? c : second ? b : a;
+}
+
 // A work group takes one token (blockIdx.x) and a run of its rows (blockIdx.y:
 // heads of q, then k, then v).  A unit is two vectors of W elements, W pairs: in the
 // half layout a thread has elements W e.. and rot/2 + W e.., otherwise 2 W e... A
@@ -85,7 +91,8 @@ __device__ __forceinline__ Words<W> pack(const float f[W]) {
 // so it is exact at any position), while the first rows are on their way.  Copies
 // (v, elements past rot) move bits.
 // Bound by reading and writing the tensors (8317 tokens, 64 + 8 + 8 heads of 128:
-// 76 us, 4.6 TB/s; with a division for each unit and its factors read for each, 98).
+// 67 us, 5.1 TB/s; with a part's fields indexed in the arguments, read for each row,
+// 79, and with a division for each unit and its factors read for each besides, 98).
 template <class Ty, int W>
 __global__ __launch_bounds__(kNT) void rope_kernel(RopeArgs a) {
   __shared__ float s_cos[PLORA_ROPE_MAX_DIM / 2], s_sin[PLORA_ROPE_MAX_DIM / 2];
@@ -97,11 +104,23 @@ __global__ __launch_bounds__(kNT) void rope_kernel(RopeArgs a) {
   const int d0 = turns && !a.interleaved ? W * e : 2 * W * e;
   const int d1 = turns && !a.interleaved ? half + W * e : 2 * W * e + W;
 
+  // (asked for before the rows, so that the angles do not wait for those)
   const int64_t ps = a.pos[t];
+  const uint64_t turns0 = tid < half ? a.turns[tid] : 0;
   const int64_t slot = a.slot ? a.slot[t] : 0;
   const bool kept = slot >= 0 && slot < a.n_slots;
   const int64_t page = slot >> a.log_page, key = slot - (page << a.log_page);
   const int64_t cell = page * a.page_stride + key * a.key_stride;
+  // (a part's fields are picked among values that the work group holds: indexed, each
+  // row would read them from memory and wait, for the rows asked for before it too)
+  const uint16_t *in0 = a.part[0].in + t * a.part[0].in_token,
+                 *in1 = a.part[1].in + t * a.part[1].in_token,
+                 *in2 = a.part[2].in + t * a.part[2].in_token;
+  uint16_t *out0 = a.part[0].out + t * a.part[0].out_token, *out1 = a.part[1].out + cell,
+           *out2 = a.part[2].out + cell;
+  const int64_t ih0 = a.part[0].in_head, ih1 = a.part[1].in_head, ih2 = a.part[2].in_head;
+  const int64_t oh0 = a.part[0].out_head, oh1 = a.part[1].out_head;
+  const int n0 = a.part[0].heads, n01 = n0 + a.part[1].heads;
   Words<W> x[kBatch], y[kBatch];
   uint16_t* to[kBatch];
   int o0[kBatch], o1[kBatch];
@@ -109,26 +128,25 @@ __global__ __launch_bounds__(kNT) void rope_kernel(RopeArgs a) {
   const auto ask = [&]() {
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      int h = row + j * step;
+      const int r = row + j * step;
       to[j] = nullptr;
-      if (idle || h >= end) continue;
-      int n = 0;
-      if (n + 1 < a.parts && h >= a.part[0].heads) h -= a.part[0].heads, n = 1;
-      if (n + 1 < a.parts && n == 1 && h >= a.part[1].heads) h -= a.part[1].heads, n = 2;
-      const Part& p = a.part[n];
-      if (p.cached && !kept) continue;
-      const uint16_t* in = p.in + t * p.in_token + h * p.in_head;
-      to[j] = p.out + (p.cached ? cell : t * p.out_token) + h * p.out_head;
-      turn[j] = turns && p.turned;
-      o0[j] = p.turned ? d0 : 2 * W * e;
-      o1[j] = p.turned ? d1 : 2 * W * e + W;
+      if (idle || r >= end) continue;
+      const bool is_k = r >= n0, is_v = r >= n01;
+      const int h = r - pick(is_v, is_k, 0, n0, n01);
+      const uint16_t* in = pick(is_v, is_k, in0, in1, in2) + h * pick(is_v, is_k, ih0, ih1, ih2);
+      turn[j] = turns && !is_v;
+      o0[j] = is_v ? 2 * W * e : d0;
+      o1[j] = is_v ? 2 * W * e + W : d1;
       x[j].v = *reinterpret_cast<const typename Unit<W>::type*>(in + o0[j]);
       y[j].v = *reinterpret_cast<const typename Unit<W>::type*>(in + o1[j]);
+      // (read whether it is kept or not, so as not to wait for the slot)
+      if (!is_k || kept)
+        to[j] = pick(is_v, is_k, out0, out1, out2) + h * pick(is_v, is_k, oh0, oh1, oh1);
     }
   };
   ask();
   for (int i = tid; i < half; i += blockDim.x) {
-    const uint64_t part = (uint64_t)ps * a.turns[i];
+    const uint64_t part = (uint64_t)ps * (i == tid ? turns0 : a.turns[i]);
     // the part of a turn, signed, in half turns: [-1, 1]
     const float f = (float)(int32_t)(part >> 32) * 0x1p-31f;
     s_cos[i] = cospif(f) * a.scale;
@@ -208,8 +226,7 @@ plora_status launch(RopeArgs& a, int32_t T, int32_t head_dim, int32_t dtype, int
   a.units = head_dim / (2 * w);
   a.rot_units = a.rot / (2 * w);
   a.log_lanes = log2_of(a.units);
-  a.rows = 0;
-  for (int n = 0; n < a.parts; ++n) a.rows += a.part[n].heads;
+  a.rows = a.part[0].heads + a.part[1].heads + a.part[2].heads;
   if (a.rows == 0) return PLORA_OK;
   const int64_t lanes = (int64_t)a.rows << a.log_lanes;
   const int threads = (int)std::min<int64_t>(kNT, (lanes + 63) / 64 * 64);
@@ -245,8 +262,7 @@ extern "C" plora_status plora_rope(const void* x, int64_t x_token, int64_t x_hea
   if (!aligned(x, 2) || !aligned(out, 2)) return PLORA_ERR_UNSUPPORTED;
   RopeArgs a{};
   a.part[0] = {(const uint16_t*)x, (uint16_t*)out, x_token, x_head, out_token, out_head,
-               heads, 1, 0};
-  a.parts = 1;
+               heads};
   a.pos = pos;
   a.turns = turns;
   a.rot = rot;
@@ -288,12 +304,11 @@ extern "C" plora_status plora_rope_append(const void* q, int64_t q_token, int64_
     return PLORA_ERR_UNSUPPORTED;
   RopeArgs a{};
   a.part[0] = {(const uint16_t*)q, (uint16_t*)q_out, q_token, q_head, out_token, out_head,
-               heads, 1, 0};
+               heads};
   a.part[1] = {(const uint16_t*)k, (uint16_t*)c.k, k_token, k_head, 0, c.head_stride,
-               c.kv_heads, 1, 1};
+               c.kv_heads};
   a.part[2] = {(const uint16_t*)v, (uint16_t*)c.v, v_token, v_head, 0, c.head_stride,
-               c.kv_heads, 0, 1};
-  a.parts = 3;
+               c.kv_heads};
   a.pos = pos;
   a.slot = slot;
   a.turns = turns;
