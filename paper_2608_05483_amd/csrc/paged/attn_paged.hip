@@ -734,12 +734,11 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
   const int t = blockIdx.x, lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
   const int e = lane % kL, sub = lane / kL;
   const int b = a.req[t], heads = a.kv_heads * a.r;
-  ReqInfo f{};
-  int R0 = 0;
-  if (b >= 0 && b < a.batch && t >= a.q_start[b] && t < a.q_start[b + 1]) {
-    f = a.info[b];
-    R0 = (t - a.q_start[b]) * a.r;
-  }
+  // (read together, of some request where there is none)
+  const int bb = min(max(b, 0), a.batch - 1);
+  const int t0 = a.q_start[bb], t1 = a.q_start[bb + 1], R0 = (t - t0) * a.r;
+  ReqInfo f = a.info[bb];
+  if (b != bb || t < t0 || t >= t1) f.state = 0;
   if (f.state == 2) return;
   const int own = f.state == 1 ? f.splits : 0;
   const int pieces = own + (f.state == 1 && f.pre_part >= 0 ? f.pre_splits : 0);
@@ -751,17 +750,29 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
     const int hd = min(h0 + sub, heads - 1), kvh = hd / a.r, R = R0 + hd % a.r;
     float M = -INFINITY, L = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    const auto place = [&](int p) {
+      const int64_t at = p < own ? (int64_t)f.part + (int64_t)p * f.rows
+                                 : (int64_t)f.pre_part + (int64_t)(p - own) * f.pre_rows + f.pre_row;
+      return (at + R) * a.kv_heads + kvh;
+    };
+    const auto piece = [&](int i) { return WIDE ? i * kWaves + wv : i; };
     for (int p0 = 0; p0 < mine; p0 += kL) {
       const int n = min(kL, mine - p0);
-      const int p = WIDE ? (p0 + e) * kWaves + wv : p0 + e;
-      int64_t at = 0;
       float m = -INFINITY, l = 0.f;
       if (e < n) {
-        at = p < own ? (int64_t)f.part + (int64_t)p * f.rows + R
-                     : (int64_t)f.pre_part + (int64_t)(p - own) * f.pre_rows + f.pre_row + R;
-        at = at * a.kv_heads + kvh;
+        const int64_t at = place(piece(p0 + e));
         m = a.pm[at], l = a.pl[at];
       }
+      // eight at a time (past the last: the last again, not added), the first before
+      // the weights are known
+      f32x4 x[kAt];
+      const auto ask = [&](int j0) {
+#pragma unroll
+        for (int j = 0; j < kAt; ++j)
+          x[j] = *reinterpret_cast<const f32x4*>(
+              a.po + place(piece(p0 + min(j0 + j, n - 1))) * D + 4 * e);
+      };
+      ask(0);
       float mx = m;
 #pragma unroll
       for (int d = kL / 2; d; d >>= 1) mx = fmaxf(mx, __shfl_xor(mx, d, 64));
@@ -777,20 +788,16 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
       for (int d = kL / 2; d; d >>= 1) s += __shfl_xor(s, d, 64);
       L = (M > -INFINITY ? L * al : L) + s;
       o *= al;
-      // eight at a time (past the last: the last again, not added)
-      for (int j0 = 0; j0 < n; j0 += kAt) {
-        f32x4 x[kAt];
-#pragma unroll
-        for (int j = 0; j < kAt; ++j) {
-          const int64_t aj = __shfl(at, min(j0 + j, n - 1), kL);
-          x[j] = *reinterpret_cast<const f32x4*>(a.po + aj * D + 4 * e);
-        }
+      for (int j0 = 0;;) {
 #pragma unroll
         for (int j = 0; j < kAt; ++j) {
           const float wj = __shfl(w, min(j0 + j, n - 1), kL);
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[i] = j0 + j < n ? fmaf(wj, x[j][i], o[i]) : o[i];
         }
+        j0 += kAt;
+        if (j0 >= n) break;
+        ask(j0);
       }
     }
     if constexpr (WIDE) {
