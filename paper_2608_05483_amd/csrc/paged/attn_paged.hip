@@ -727,11 +727,11 @@ __global__ __launch_bounds__(kNT, 2) void items_kernel(AttnArgs a) {
 // items wrote themselves are left, rows without a key get zeros.  Bound by reading
 // the partials, or by the latency of its chain of loads.
 template <class Ty, int D, bool WIDE>
-__global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
+__device__ __forceinline__ void merge_token(const AttnArgs& a, int t, int32_t per) {
   constexpr int kL = D / 4, kRows = 64 / kL, kAt = 8;
   __shared__ f32x4 s_o[WIDE ? kWaves : 1][64];
   __shared__ float s_m[WIDE ? kWaves : 1][kRows], s_l[WIDE ? kWaves : 1][kRows];
-  const int t = blockIdx.x, lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
   const int e = lane % kL, sub = lane / kL;
   const int b = a.req[t], heads = a.kv_heads * a.r;
   // (read together, of some request where there is none)
@@ -836,6 +836,31 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
   }
 }
 
+// Many tokens are kMergeTokens work groups' in turn, which look at 64 of theirs at
+// once, a lane each, for those that have something to merge: few do among the tokens
+// of long prompts, and those of one request lie with different work groups (16247
+// tokens, none of them: 10.3 us with a work group each, 4.8 so).
+constexpr int kMergeTokens = 2048;
+template <class Ty, int D, bool WIDE>
+__global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
+  const int n = gridDim.x, lane = threadIdx.x & 63;
+  if (n >= a.T) return merge_token<Ty, D, WIDE>(a, blockIdx.x, per);
+  for (int t0 = blockIdx.x; t0 < a.T; t0 += 64 * n) {
+    const int t = t0 + lane * n;
+    bool any = false;
+    if (t < a.T) {
+      const int b = a.req[t];
+      any = b < 0 || b >= a.batch || a.info[b].state != 2;
+    }
+    uint64_t mask = __ballot(any);
+    while (mask) {
+      const int i = __builtin_ctzll(mask);
+      mask &= mask - 1;
+      merge_token<Ty, D, WIDE>(a, t0 + i * n, per);
+    }
+  }
+}
+
 struct WsLayout {
   size_t l, o, bytes;
 };
@@ -881,8 +906,9 @@ plora_status launch(const AttnArgs& a, const Bounds& b, int64_t pool_bytes, hipS
                        dim3(kNT), 0, stream, a, rows);
   } else {
     const int per = a.T < 512 ? kWaves * rows : heads;
-    hipLaunchKernelGGL((merge_kernel<Ty, D, false>), dim3(a.T, (heads + per - 1) / per),
-                       dim3(kNT), 0, stream, a, per);
+    hipLaunchKernelGGL((merge_kernel<Ty, D, false>),
+                       dim3(std::min(a.T, kMergeTokens), (heads + per - 1) / per), dim3(kNT), 0,
+                       stream, a, per);
   }
   return launch_status();
 }

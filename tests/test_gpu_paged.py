@@ -299,6 +299,27 @@ def check(got, ref, size, dt, keys, vmax=6.0):
     assert worst <= 0, worst
 
 
+@pytest.mark.parametrize("long", [2100, 4100])
+def test_few_tokens_to_merge_among_many(G, P, long):
+    """A long prompt, whose rows no partials make, between requests that share a
+    prefix, requests of no group and padding, over more tokens than the merge has
+    work groups."""
+    B = 24
+    new = np.where(np.arange(B) % 5 == 4, 3, 1)
+    new[B // 2] = long
+    group = np.arange(B) % 3 - 1
+    group[B // 2] = -1
+    b = Batch(G, P, [96 + 7 * i for i in range(B)], new, 4, 2, 64, group=group, prefix=[64, 96],
+              pad=133, seed=long)
+    got = b.run(0.125)
+    start = b.step.q_start.cpu().numpy()
+    lo, hi = start[B // 2], start[B // 2 + 1]
+    rows = np.r_[0:lo + 3, lo + 2040:lo + 2060, hi - 3:len(got)]
+    ref, size = b.ref(0.125, rows)
+    check(got[rows], ref[rows], size[rows], BF, 6000)
+    assert (got[start[-1]:] == 0).all()
+
+
 @pytest.mark.parametrize("D", [128, 64])
 @pytest.mark.parametrize("new", [1, 40])
 def test_many_keys_of_little_weight_fp16(G, P, D, new):
