@@ -231,9 +231,10 @@ def rope_append(q, k, v, pos, slot, turns, cache: KVCache, q_out, layout: str = 
     pk, kt, kh = _heads("k", k, dt)
     pv, vt, vh = _heads("v", v, dt)
     po, ot, oh = _heads("q_out", q_out, dt)
-    T, H, D = q.shape
-    if D != cache.head_dim or q_out.shape != q.shape or k.shape != (T, cache.kv_heads, D) or \
-            v.shape != k.shape:
+    shape, kv_shape = q.shape, k.shape
+    T, H, D = shape
+    if D != cache.head_dim or q_out.shape != shape or kv_shape != (T, cache.kv_heads, D) or \
+            v.shape != kv_shape:
         raise ValueError("q, k, v, q_out: shapes do not fit each other and the cache")
     _ok("plora_rope_append", lib.plora_rope_append(
         pq, qt, qh, pk, kt, kh, pv, vt, vh, _ints("pos", pos, _I32, T),
