@@ -723,7 +723,7 @@ __global__ __launch_bounds__(kNT, 2) void items_kernel(AttnArgs a) {
 // D / 4 pieces are found at once, a lane a piece, then eight partials are asked for
 // at a time.  WIDE: four wavefronts for the same rows, a quarter of the pieces each,
 // joined in a fixed order (few rows, cut into many pieces: one request of 30011 keys
-// x 64 heads, 59 pieces: 10.0 us with a wavefront a row, 5.7 so).  Rows that the
+// x 64 heads, 59 pieces: 10.0 us with a wavefront a row, 5.4 so).  Rows that the
 // items wrote themselves are left, rows without a key get zeros.  Bound by reading
 // the partials, or by the latency of its chain of loads.
 template <class Ty, int D, bool WIDE>
