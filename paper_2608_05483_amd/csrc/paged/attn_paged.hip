@@ -849,8 +849,8 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
     const int t = t0 + lane * n;
     bool any = false;
     if (t < a.T) {
-      const int b = a.req[t];
-      any = b < 0 || b >= a.batch || a.info[b].state != 2;
+      const int b = a.req[t], bb = min(max(b, 0), a.batch - 1);
+      any = b != bb || t < a.q_start[bb] || t >= a.q_start[bb + 1] || a.info[bb].state != 2;
     }
     uint64_t mask = __ballot(any);
     while (mask) {
