@@ -424,9 +424,10 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
 // whether that still stands: it is only raised, the output rescaled and the weights
 // formed again, if a lane's sum of 32 passes kBar (bf16 2^13; fp16 2^16, above which
 // a weight becomes infinite and the sum with it).  So no maximum is looked for in
-// most steps, and no weight is more than its type holds.  The weights are summed as rounded to the type, which they are for the
-// product with V: its rounding errors average out below the output's own, and a
-// second product for the rest would add half to the work that bounds the kernel.
+// most steps, and no weight is more than its type holds.  The weights are summed as
+// rounded to the type, which they are for the product with V: its rounding errors
+// average out below the output's own, and a second product for the rest would add
+// half to the work that bounds the kernel.
 // Bound by the matrix units and what they cannot hide: for 64 keys and 32 rows 32
 // products (1024 cycles), 64 vector instructions and 32 exponentials (512), 64 reads
 // of LDS (about 600).  64 keys x 128 rows, two work groups on every compute unit:
@@ -751,8 +752,9 @@ __device__ __forceinline__ void merge_token(const AttnArgs& a, int t, int32_t pe
     float M = -INFINITY, L = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     const auto place = [&](int p) {
-      const int64_t at = p < own ? (int64_t)f.part + (int64_t)p * f.rows
-                                 : (int64_t)f.pre_part + (int64_t)(p - own) * f.pre_rows + f.pre_row;
+      const int64_t at =
+          p < own ? (int64_t)f.part + (int64_t)p * f.rows
+                  : (int64_t)f.pre_part + (int64_t)(p - own) * f.pre_rows + f.pre_row;
       return (at + R) * a.kv_heads + kvh;
     };
     const auto piece = [&](int i) { return WIDE ? i * kWaves + wv : i; };

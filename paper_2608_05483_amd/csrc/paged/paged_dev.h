@@ -21,10 +21,10 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 
-// The two 16-bit types: unpacking, rounding to nearest even.  kLift: the power of two by which
-// softmax weights are raised where they are held in the type, kTileLift where they
-// may grow to kBar in sum before the maximum is looked at again: fp16 loses what is
-// below 2^-25, and many keys of such weights beside one of weight 1 still count.
+// The two 16-bit types: unpacking, rounding to nearest even.  kLift: the power of two
+// by which softmax weights are raised where they are held in the type, kTileLift where
+// they may grow to kBar in sum before the maximum is looked at again: fp16 loses what
+// is below 2^-25, and many keys of such weights beside one of weight 1 still count.
 struct Bf16 {
   static constexpr float kLift = 0.f, kTileLift = 0.f, kBar = 8192.f;
   __device__ static __forceinline__ float lo(uint32_t w) { return __uint_as_float(w << 16); }
