@@ -814,13 +814,12 @@ __device__ __forceinline__ void merge_token(const AttnArgs& a, int t, int32_t pe
         o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
+          // (without a maximum: scores of -inf, which weigh nothing beside others, or NaN,
+          // which the sums below still carry through a weight of zero)
           const float mw = s_m[w][sub], lw = s_l[w][sub];
-          if (mw == -INFINITY) {
-            if (M == -INFINITY) L += lw;
-            continue;
-          }
-          const float g = exp2_(mw - M);
-          L = fmaf(g, lw, L);
+          const float g = mw == -INFINITY ? 0.f : exp2_(mw - M);
+          if (mw > -INFINITY) L = fmaf(g, lw, L);
+          else if (M == -INFINITY) L += lw;
           const f32x4 x = s_o[w][lane];
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[i] = fmaf(g, x[i], o[i]);
