@@ -203,12 +203,13 @@ plora_status plora_attn_plan(const plora_kv_step* step, const plora_attn_shape* 
  * j <= pos_t of token t's request.  A row with no key (padding, a request left
  * out) gets zeros; a key that a row does not see has no part in it, whatever its
  * values.  q_token, q_head, out_token, out_head: element strides (multiples of
- * 8), pointers 16-byte aligned, cache strides multiples of 8, one page's heads
- * within 2^31 bytes.  Scores, weights and sums are fp32; the weights enter the
- * product with v as two values of the type (16 bits) where a tile has up to 16
- * rows, as one above, where that product bounds the call.  plan: as
- * plora_attn_plan wrote it for the same step and shape; ws: at least
- * plora_attn_paged_workspace_bytes bytes, 16-byte aligned, no contents needed.
+ * 8), pointers 16-byte aligned, cache strides multiples of 8, the token stride
+ * from head_dim to below 2^25 (a pool may have its pages, heads and keys in any
+ * order).  Scores, weights and sums are fp32; the weights enter the product with
+ * v as two values of the type (16 bits) where a tile has up to 16 rows, as one
+ * above, where that product bounds the call.  plan: as plora_attn_plan wrote it
+ * for the same step and shape; ws: at least plora_attn_paged_workspace_bytes
+ * bytes, 16-byte aligned, no contents needed.
  */
 plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t q_head,
                               const plora_kv_cache* cache, const plora_kv_step* step,

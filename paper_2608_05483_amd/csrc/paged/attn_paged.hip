@@ -60,6 +60,10 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 // Where 16 keys of one page and head lie, and how many bytes of them a row may
 // read: what lies past the valid rows, or in a page outside the pool, reads zero
 // through the buffer resource and fetches nothing.
+// (What the 16 keys span, and a lane's offset in it, are counted in 32 bits: at most
+// 30 token strides in bytes.)
+constexpr int64_t kTokenStrideEnd = INT64_C(1) << 25;
+static_assert(30 * kTokenStrideEnd + 4096 <= INT32_MAX, "");
 struct Cell {
   int64_t at;
   int bytes;
@@ -74,7 +78,7 @@ __device__ __forceinline__ Cell cell_of(const AttnArgs& a, int page, int kvh, in
   page = ok ? page : 0;
   Cell c;
   c.at = page * a.page_stride + kvh * a.head_stride +
-         (key & ((1 << a.log_page) - 1)) * a.key_stride;
+         (int64_t)(key & ((1 << a.log_page) - 1)) * a.key_stride;
   c.bytes = ok ? ((min(end - key, 16) - 1) * a.key_stride + D) * 2 : 0;
   return c;
 }
@@ -510,7 +514,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
     const int key = k0 + 16 * lane;
     const bool ok = page >= 0 && page < a.n_pages && key < end;
     const int64_t at = (ok ? page : 0) * a.page_stride + kvh * a.head_stride +
-                       (key & ((1 << a.log_page) - 1)) * a.key_stride;
+                       (int64_t)(key & ((1 << a.log_page) - 1)) * a.key_stride;
     at_lo = (int)at, at_hi = (int)(at >> 32);
     bytes = ok ? ((min(end - key, 16) - 1) * a.key_stride + D) * 2 : 0;
     ask(k0 + 1024);
@@ -945,7 +949,7 @@ extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t
   if (shape_empty(s)) return PLORA_OK;
   if (c.token_stride < s.head_dim) return PLORA_ERR_INVALID_ARG;
   if (q_token % 8 || q_head % 8 || out_token % 8 || out_head % 8 || c.page_stride % 8 ||
-      c.head_stride % 8 || c.token_stride % 8 || c.token_stride > (INT32_MAX / 4) / 16)
+      c.head_stride % 8 || c.token_stride % 8 || c.token_stride >= kTokenStrideEnd)
     return PLORA_ERR_UNSUPPORTED;
   if (!q || !out || !plan || !ws || !step->pos || !step->req || !step->q_start ||
       (c.n_pages > 0 && (!c.k || !c.v)) || (step->max_pages > 0 && !step->table))

@@ -348,3 +348,11 @@ def _constant(name):
 
 
 FEW_TARGET, TILE_TARGET = _constant("kFewTarget"), _constant("kTileTarget")
+
+
+@pytest.mark.parametrize("page", [16, 128, 256])
+def test_longest_token_stride(page):
+    """A cache's keys may lie up to 2^25 elements apart, whatever the page size."""
+    for stride, want in ((1 << 25, UNS), ((1 << 25) - 8, SMALL)):
+        assert attn_status(c=cache(page_size=page, token_stride=stride), s=step(page_size=page),
+                           wb=64) == want
