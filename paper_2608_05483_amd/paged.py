@@ -5,7 +5,8 @@ pages, cache slots) and ``attn_plan`` its attention; in every layer
 ``rope_append`` turns q and k and stores k and v, and ``attn_paged`` attends.  As
 in ``plora``, the functions forward device pointers, strides and the caller's
 stream to the C ABI and raise ``PloraError`` on a non-OK status; the classes hold
-the buffers a step needs as torch tensors.
+the buffers a step needs as torch tensors.  Tensors of another type, shape or device
+than a call takes are refused before it (TypeError, ValueError).
 
 ``rope_turns`` gives the rotation's frequencies, scaled for long contexts where
 asked; ``run_layers`` runs a step's layers as a serving loop would.
@@ -85,13 +86,16 @@ _I32, _I64 = torch.int32, torch.int64
 _current = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream, t) -> int:
-    """The stream given, or the current one of the tensor's device."""
+def _stream(stream, dev: int) -> int:
+    """The stream given, or the current one of GPU dev, which all tensors of the
+    call are on (-1: they are the host's, whose addresses no kernel may get)."""
+    if dev < 0:
+        raise ValueError("GPU tensors expected")
     if stream is not None:
         return int(stream.cuda_stream)
     if _current is not None:
-        return _current(t.get_device())
-    return int(torch.cuda.current_stream(t.device).cuda_stream)
+        return _current(dev)
+    return int(torch.cuda.current_stream(dev).cuda_stream)
 
 
 def _ok(fn: str, status: int) -> None:
@@ -106,19 +110,28 @@ def _dtype(t) -> int:
     return code
 
 
-def _heads(name: str, t, dtype: int):
-    """Pointer, token stride and head stride of a [T, heads, dim] tensor."""
+def _on(name: str, t, dev: int) -> None:
+    if t.get_device() != dev:
+        raise ValueError(f"{name}: on another device than the call's other tensors")
+
+
+def _heads(name: str, t, dtype: int, dev: int):
+    """Pointer, token stride and head stride of a [T, heads, dim] tensor on dev."""
     s = t.stride()
     if len(s) != 3 or (s[2] != 1 and t.shape[2] > 1):
         raise ValueError(f"{name}: a [T, heads, dim] tensor with contiguous dim expected")
     if _CODE.get(t.dtype) != dtype:
         raise TypeError(f"{name}: has another type than expected")
+    if t.get_device() != dev:
+        _on(name, t, dev)
     return t.data_ptr(), s[0], s[1]
 
 
-def _ints(name: str, t, dtype, n: int):
+def _ints(name: str, t, dtype, n: int, dev: int):
     if t.dtype is not dtype or t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous {dtype} tensor of at least {n} entries expected")
+    if t.get_device() != dev:
+        _on(name, t, dev)
     return t.data_ptr()
 
 
@@ -131,6 +144,8 @@ class KVCache:
             raise ValueError("k and v: 4-d tensors of one shape, type and strides expected")
         if k.shape[3] > 1 and k.stride(3) != 1:
             raise ValueError("k and v: contiguous head_dim expected")
+        self.dev = k.get_device()
+        _on("v", v, self.dev)
         self.k, self.v = k, v
         self.n_pages, self.kv_heads, self.page_size, self.head_dim = k.shape
         self.dtype = _dtype(k)
@@ -156,8 +171,9 @@ class Step:
         self.batch, self.T, self.page_size, self.max_pages = batch, T, page_size, max_pages
         i32 = dict(dtype=torch.int32, device=device)
         self.table = table if table is not None else torch.zeros((batch, max_pages), **i32)
-        _ints("table", self.table, _I32, batch * max_pages)
         self.q_start = torch.zeros(batch + 1, **i32)
+        self.dev = self.q_start.get_device()
+        _ints("table", self.table, _I32, batch * max_pages, self.dev)
         self.kv_len = torch.zeros(batch, **i32)
         self.pos = torch.zeros(T, **i32)
         self.req = torch.full((T,), -1, **i32)
@@ -183,6 +199,7 @@ class AttnPlan:
         u8 = dict(dtype=torch.uint8, device=device)
         self.plan = torch.zeros(attn_plan_bytes(self.shape), **u8)
         self.ws = torch.empty(attn_paged_workspace_bytes(self.shape), **u8)
+        self.dev = self.ws.get_device()
 
 
 def attn_plan_bytes(shape: plora_attn_shape) -> int:
@@ -199,12 +216,12 @@ def attn_paged_workspace_bytes(shape: plora_attn_shape) -> int:
 def kv_plan(past, n_new, free_pages, free_head, free_next, step: Step, stream=None) -> None:
     """past, n_new int32 [batch]; free_pages int32, handed out from entry
     free_head[0] on; free_next[0] is the entry after."""
-    n = step.batch
+    n, dev = step.batch, step.dev
     _ok("plora_kv_plan", lib.plora_kv_plan(
-        _ints("past", past, _I32, n), _ints("n_new", n_new, _I32, n),
-        _ints("free_pages", free_pages, _I32, 0), free_pages.numel(),
-        _ints("free_head", free_head, _I32, 1), _ints("free_next", free_next, _I32, 1),
-        step.ref, _stream(stream, past)))
+        _ints("past", past, _I32, n, dev), _ints("n_new", n_new, _I32, n, dev),
+        _ints("free_pages", free_pages, _I32, 0, dev), free_pages.numel(),
+        _ints("free_head", free_head, _I32, 1, dev), _ints("free_next", free_next, _I32, 1, dev),
+        step.ref, _stream(stream, dev)))
 
 
 def rope(x, pos, turns, out, layout: str = "half", scale: float = 1.0, inverse: bool = False,
@@ -213,59 +230,64 @@ def rope(x, pos, turns, out, layout: str = "half", scale: float = 1.0, inverse: 
     inverse gives the input's gradient from the output's."""
     if out.shape != x.shape:
         raise ValueError("out: x's shape expected")
-    dt = _dtype(x)
-    px, xt, xh = _heads("x", x, dt)
-    po, ot, oh = _heads("out", out, dt)
+    dt, dev = _dtype(x), x.get_device()
+    px, xt, xh = _heads("x", x, dt, dev)
+    po, ot, oh = _heads("out", out, dt, dev)
     T, H, D = x.shape
     _ok("plora_rope", lib.plora_rope(
-        px, xt, xh, _ints("pos", pos, _I32, T), _ints("turns", turns, _I64, 0), T, H, D,
-        2 * turns.numel(), _LAYOUT[layout], scale, inverse, dt, po, ot, oh, _stream(stream, x)))
+        px, xt, xh, _ints("pos", pos, _I32, T, dev), _ints("turns", turns, _I64, 0, dev), T, H, D,
+        2 * turns.numel(), _LAYOUT[layout], scale, inverse, dt, po, ot, oh, _stream(stream, dev)))
 
 
 def rope_append(q, k, v, pos, slot, turns, cache: KVCache, q_out, layout: str = "half",
                 scale: float = 1.0, stream=None) -> None:
     """q, q_out [T, heads, dim], k, v [T, kv_heads, dim], pos int32 [T], slot
     int64 [T]: q turned into q_out, k turned into the cache, v stored there."""
-    dt = cache.dtype
-    pq, qt, qh = _heads("q", q, dt)
-    pk, kt, kh = _heads("k", k, dt)
-    pv, vt, vh = _heads("v", v, dt)
-    po, ot, oh = _heads("q_out", q_out, dt)
+    dt, dev = cache.dtype, cache.dev
+    pq, qt, qh = _heads("q", q, dt, dev)
+    pk, kt, kh = _heads("k", k, dt, dev)
+    pv, vt, vh = _heads("v", v, dt, dev)
+    po, ot, oh = _heads("q_out", q_out, dt, dev)
     shape, kv_shape = q.shape, k.shape
     T, H, D = shape
     if D != cache.head_dim or q_out.shape != shape or kv_shape != (T, cache.kv_heads, D) or \
             v.shape != kv_shape:
         raise ValueError("q, k, v, q_out: shapes do not fit each other and the cache")
     _ok("plora_rope_append", lib.plora_rope_append(
-        pq, qt, qh, pk, kt, kh, pv, vt, vh, _ints("pos", pos, _I32, T),
-        _ints("slot", slot, _I64, T), _ints("turns", turns, _I64, 0), T, H, 2 * turns.numel(),
-        _LAYOUT[layout], scale, cache.ref, po, ot, oh, _stream(stream, q)))
+        pq, qt, qh, pk, kt, kh, pv, vt, vh, _ints("pos", pos, _I32, T, dev),
+        _ints("slot", slot, _I64, T, dev), _ints("turns", turns, _I64, 0, dev), T, H,
+        2 * turns.numel(), _LAYOUT[layout], scale, cache.ref, po, ot, oh, _stream(stream, dev)))
 
 
 def attn_plan(step: Step, plan: AttnPlan, segs=None, prefix_len=None, stream=None) -> None:
     """segs: the batch's groups (plora.Segments filled by plora.segment from a
     group id per request); prefix_len int32 [n_groups]."""
-    groups, lens, n = None, None, 0
+    groups, lens, n, dev = None, None, 0, step.dev
+    _on("plan", plan.ws, dev)
     if segs is not None:
+        _on("segs", segs.perm, dev)
         groups, n = ctypes.byref(segs.struct), segs.n_adapters
     if prefix_len is not None:
-        lens = _ints("prefix_len", prefix_len, _I32, n)
+        lens = _ints("prefix_len", prefix_len, _I32, n, dev)
     _ok("plora_attn_plan", lib.plora_attn_plan(
         step.ref, plan.ref, groups, lens, n, plan.plan.data_ptr(), plan.plan.numel(),
-        _stream(stream, plan.plan)))
+        _stream(stream, dev)))
 
 
 def attn_paged(q, cache: KVCache, step: Step, plan: AttnPlan, scale: float, out,
                stream=None) -> None:
     """q, out [T, heads, head_dim]."""
-    dt = cache.dtype
-    pq, qt, qh = _heads("q", q, dt)
-    po, ot, oh = _heads("out", out, dt)
+    dt, dev = cache.dtype, cache.dev
+    pq, qt, qh = _heads("q", q, dt, dev)
+    po, ot, oh = _heads("out", out, dt, dev)
     if q.shape != plan.q_shape or out.shape != plan.q_shape:
         raise ValueError("q, out: the plan's [T, heads, head_dim] expected")
+    if step.dev != dev or plan.dev != dev:
+        raise ValueError("step, plan: on another device than the cache")
     _ok("plora_attn_paged", lib.plora_attn_paged(
         pq, qt, qh, cache.ref, step.ref, plan.ref, scale, plan.plan.data_ptr(),
-        plan.plan.numel(), po, ot, oh, plan.ws.data_ptr(), plan.ws.numel(), _stream(stream, q)))
+        plan.plan.numel(), po, ot, oh, plan.ws.data_ptr(), plan.ws.numel(),
+        _stream(stream, dev)))
 
 
 # ---- the rotation's frequencies ---------------------------------------------------

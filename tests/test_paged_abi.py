@@ -356,3 +356,21 @@ def test_longest_token_stride(page):
     for stride, want in ((1 << 25, UNS), ((1 << 25) - 8, SMALL)):
         assert attn_status(c=cache(page_size=page, token_stride=stride), s=step(page_size=page),
                            wb=64) == want
+
+
+def test_binding_refuses_host_tensors():
+    """No call hands the address of a host tensor to a kernel."""
+    import torch
+    z = lambda *s, dt=torch.bfloat16: torch.zeros(s, dtype=dt)
+    i = lambda n, dt=torch.int32: torch.zeros(n, dtype=dt)
+    c = G.KVCache(z(3, 2, 16, 64), z(3, 2, 16, 64))
+    s = G.Step(2, 5, 16, 4, device="cpu")
+    p = G.AttnPlan(s, 4, 2, 64, max_q=3, device="cpu")
+    q, k = z(5, 4, 64), z(5, 2, 64)
+    turns = i(32, torch.int64)
+    for call in (lambda: G.kv_plan(i(2), i(2), i(3), i(1), i(1), s),
+                 lambda: G.rope(q, i(5), turns, q),
+                 lambda: G.rope_append(q, k, k, i(5), i(5, torch.int64), turns, c, q),
+                 lambda: G.attn_plan(s, p), lambda: G.attn_paged(q, c, s, p, 0.1, q.clone())):
+        with pytest.raises(ValueError, match="GPU tensors"):
+            call()
