@@ -157,7 +157,7 @@ plora_status plora_rope_append(const void* q, int64_t q_token, int64_t q_head,
  *              h / (heads / kv_heads)
  *   head_dim   64 or 128
  *   max_q      an upper bound on every request's new tokens (a request with
- *              more gets zeros)
+ *              more gets zeros, and plora_attn_plan counts it)
  *   shared     nonzero if plora_attn_plan will be given groups
  */
 typedef struct {
@@ -191,8 +191,15 @@ size_t plora_attn_paged_workspace_bytes(const plora_attn_shape* shape);
  * PLORA_ATTN_SHARE_ROWS query rows per key head (one with more fills the matrix
  * units by itself), and another request of its group does.  Without groups seg
  * and prefix_len are NULL.  One launch.
+ *
+ * int32 word PLORA_ATTN_PLAN_LEFT_OUT of the plan is the number of requests that
+ * have tokens in the step and are left out here, their outputs zeros: those of
+ * more than max_q tokens, and those whose lengths do not agree with the step's
+ * or the shape's bounds.  (Requests that plora_kv_plan left out are counted in
+ * its meta.)
  */
 #define PLORA_ATTN_SHARE_ROWS 128
+#define PLORA_ATTN_PLAN_LEFT_OUT 6
 plora_status plora_attn_plan(const plora_kv_step* step, const plora_attn_shape* shape,
                              const plora_segments* seg, const int32_t* prefix_len,
                              int32_t n_groups, void* plan, size_t plan_bytes,

@@ -99,7 +99,9 @@ struct PlanHeader {
   int32_t part_rows;
   int32_t few_keys, tile_keys; // keys per piece
   int32_t later;               // short items of few rows, from their list's end
+  int32_t left;                // requests whose tokens get zeros
 };
+static_assert(offsetof(PlanHeader, left) == 4 * PLORA_ATTN_PLAN_LEFT_OUT, "");
 
 inline bool shape_ok(const plora_attn_shape& s) {
   return s.batch >= 0 && s.T >= 0 && s.heads >= 0 && s.kv_heads >= 0 && s.max_q >= 0 &&

@@ -159,7 +159,7 @@ __device__ __forceinline__ int per_piece(double work, int target, int kv_heads, 
 __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
   __shared__ int32_t s_kept[kKeptArrays * (kHere + 1)];
   __shared__ Set s_sets[kNT];
-  __shared__ int s_keys[kNT], s_tiles[kNT], s_big[kNT], s_bigs;
+  __shared__ int s_keys[kNT], s_tiles[kNT], s_big[kNT], s_bigs, s_left;
   __shared__ uint32_t red1[kWaves][1], red4[kWaves][4];
   __shared__ double s_work[kWaves][2];
   __shared__ int64_t s_cost[kTries];
@@ -172,7 +172,8 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
     y = Kept{p, p + n, p + 2 * n, p + 3 * n, p + 4 * n, p + 5 * n, p + 6 * n,
              p + 7 * n, p + 8 * n, p + 9 * n, p + 10 * n, p + 11 * n};
   }
-  int n_seg = 0, n_valid = 0, b0 = -1;
+  int n_seg = 0, n_valid = 0, b0 = -1, left = 0;
+  if (tid == 0) s_left = 0;
   if (a.shared) {
     n_seg = min(max(a.meta[0], 0), a.cap);
     n_valid = min(max(a.meta[1], 0), a.batch);
@@ -182,7 +183,9 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
     const int q0 = a.q_start[b], q1 = a.q_start[b + 1], kv = a.kv_len[b];
     int n = 0;
     if (q0 >= 0 && q0 < q1 && q1 <= a.T && a.req[q0] == b) n = q1 - q0;
-    y.n[b] = n > a.max_q || kv < n || kv > a.max_keys ? 0 : n;
+    const bool fits = n <= a.max_q && kv >= n && kv <= a.max_keys;
+    left += n > 0 && !fits;
+    y.n[b] = fits ? n : 0;
     y.q0[b] = q0;
     y.kv[b] = kv;
     y.u[b] = 0;
@@ -380,6 +383,7 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
         f.pre_row = (y.place[b] - tok) * a.r;
         if (f.pre_part < 0) f.state = 0;
       }
+      left += y.n[b] > 0 && f.state == 0;
       a.info[b] = f;
     }
     const int bigs = s_bigs;
@@ -391,8 +395,11 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
     }
     __syncthreads();
   }
+  if (left > 0) atomicAdd(&s_left, left);
+  __syncthreads();
   if (tid == 0) {
     PlanHeader h{};
+    h.left = s_left;
     h.few = min((int)sum[0], a.few_cap);
     h.later = min((int)sum[3], a.few_cap - h.few);
     h.tiles = min((int)sum[1], a.tile_cap);

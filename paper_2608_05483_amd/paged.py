@@ -28,6 +28,7 @@ MAX_BATCH = 16384
 MAX_TOKENS = 1 << 20
 PAGE_MIN, PAGE_MAX = 16, 256
 SHARE_ROWS = 128
+PLAN_LEFT_OUT = 6
 
 EXPORTED = ("plora_kv_plan", "plora_rope", "plora_rope_append", "plora_attn_plan_bytes",
             "plora_attn_paged_workspace_bytes", "plora_attn_plan", "plora_attn_paged")
@@ -200,6 +201,14 @@ class AttnPlan:
         self.plan = torch.zeros(attn_plan_bytes(self.shape), **u8)
         self.ws = torch.empty(attn_paged_workspace_bytes(self.shape), **u8)
         self.dev = self.ws.get_device()
+
+    @property
+    def left_out(self):
+        """int32 [1] on the GPU: the requests whose tokens the plan last laid out
+        leaves out, their outputs zeros (more than max_q of them, say)."""
+        if self.plan.numel() == 0:
+            return torch.zeros(1, dtype=torch.int32, device=self.plan.device)
+        return self.plan[4 * PLAN_LEFT_OUT:4 * PLAN_LEFT_OUT + 4].view(torch.int32)
 
 
 def attn_plan_bytes(shape: plora_attn_shape) -> int:

@@ -374,3 +374,9 @@ def test_binding_refuses_host_tensors():
                  lambda: G.attn_plan(s, p), lambda: G.attn_paged(q, c, s, p, 0.1, q.clone())):
         with pytest.raises(ValueError, match="GPU tensors"):
             call()
+
+
+def test_the_plan_s_count_is_where_the_header_says():
+    text = open(HEADER).read()
+    assert int(re.search(r"#define PLORA_ATTN_PLAN_LEFT_OUT (\d+)", text).group(1)) == \
+        G.PLAN_LEFT_OUT
