@@ -22,7 +22,7 @@ def kv_plan(past, new, free, head, table, page, T):
         q_start.append(min(at, T))
         start = at
         at = min(at + max(n, 0), T + 1)
-        ok = p >= 0 and n >= 0 and p + n <= max_pages * page and at <= T
+        ok = p >= 0 and n >= 0 and p + n <= max_pages * page and (at <= T or n == 0)
         need = -(-(p + n) // page) - -(-p // page) if ok else 0
         if ok and need > 0:
             ok = want + need <= avail

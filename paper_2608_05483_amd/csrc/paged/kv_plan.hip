@@ -87,7 +87,7 @@ __global__ __launch_bounds__(kNT) void kv_plan_kernel(
     for (int i = 0; i < kPer; ++i) {
       st[i] = at;
       at = min(at + min(max(n[i], 0), T + 1), T + 1);
-      if (at > T) need[i] = -1;
+      if (at > T && n[i] != 0) need[i] = -1;
     }
     tok_carry = min(tok_carry + (int)total[0], T + 1);
     if (tok_carry > T) {

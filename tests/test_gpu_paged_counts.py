@@ -6,7 +6,8 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
-from test_gpu_paged import BF, G, P, Batch, check, i32  # noqa: E402, F401
+from test_gpu_paged import (BF, G, P, Batch, check, check_plan, i32,  # noqa: E402, F401
+                            run_plan)
 
 
 def test_requests_that_the_plan_leaves_out(G, P):
@@ -49,3 +50,17 @@ def test_an_empty_plan_leaves_none_out(G, P):
     plan = G.AttnPlan(step, 4, 2, 64, max_q=1)
     G.attn_plan(step, plan)
     assert plan.left_out.tolist() == [0]
+
+
+def test_requests_of_no_tokens_behind_too_many(G, P):
+    """Tokens that pass the step's rows are left out with their requests; a request
+    that brings none keeps its length and is not one of them, in the first chunk of
+    requests and in a later one."""
+    for n in (4, 1100):
+        past, new = np.full(n, 16), np.zeros(n, int)
+        new[1] = 30
+        got, _ = run_plan(G, past, new, np.arange(9), 0, np.zeros((n, 4), int), 16, 20)
+        assert list(got["meta"][:3]) == [20, 0, 1]
+        assert (got["kv_len"] == 16).all() and (got["req"] == -1).all()
+        assert list(got["q_start"]) == [0, 0] + [20] * (n - 1)
+        check_plan(G, past, new, np.arange(9), 0, np.zeros((n, 4), int), 16, 20)

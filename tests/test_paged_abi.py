@@ -380,3 +380,8 @@ def test_the_plan_s_count_is_where_the_header_says():
     text = open(HEADER).read()
     assert int(re.search(r"#define PLORA_ATTN_PLAN_LEFT_OUT (\d+)", text).group(1)) == \
         G.PLAN_LEFT_OUT
+
+
+def test_oracle_keeps_requests_of_no_tokens():
+    r = OP.kv_plan([16, 16, 16], [0, 30, 0], [1, 2, 3], 0, np.zeros((3, 4), int), 16, 20)
+    assert r["meta"][:3] == [20, 0, 1] and r["kv_len"] == [16, 16, 16]
