@@ -99,20 +99,21 @@ def _asan_object(src: str, verbose: bool) -> str:
 
 
 def build_asan(verbose: bool = False) -> str:
-    """The host side (plora.hip: argument checks, workspace layout, plans)
+    """The files with entry points (argument checks, workspace layouts, plans)
     compiled with the sanitizer, linked with the product build's objects of
-    the kernel files (whose host code is their launchers), built if absent."""
-    host = os.path.join(CSRC, "plora.hip")
-    others = [s for s in SRCS if s != host]
+    the kernel files (``k_*.hip``, whose host code is their launchers), built if
+    absent."""
+    others = [s for s in SRCS if os.path.basename(s).startswith("k_")]
+    host = [s for s in SRCS if s not in others]
     objs = [os.path.join(OBJ_DIR, os.path.basename(s) + ".o") for s in others]
     missing = [s for s, o in zip(others, objs) if not os.path.exists(o)]
     with ThreadPoolExecutor(max_workers=jobs()) as ex:
-        futs = [ex.submit(_asan_object, host, verbose)] + \
-               [ex.submit(_object, s, verbose) for s in missing]
-        asan_host = futs[0].result()
-        for f in futs[1:]:
+        futs = [ex.submit(_asan_object, s, verbose) for s in host]
+        rest = [ex.submit(_object, s, verbose) for s in missing]
+        asan = [f.result() for f in futs]
+        for f in rest:
             f.result()
-    return _link([asan_host] + objs, ASAN_LIB, verbose)
+    return _link(asan + objs, ASAN_LIB, verbose)
 
 
 if __name__ == "__main__":
