@@ -33,7 +33,9 @@
  * pointer, a negative size or stride, or sizes that do not fit each other;
  * PLORA_ERR_UNSUPPORTED for what lies outside the stated ranges or alignments;
  * PLORA_ERR_WORKSPACE_TOO_SMALL; PLORA_ERR_HIP for a failed launch.  T, batch or
- * heads of 0 is a no-op (plora_kv_plan still writes its per-request outputs).
+ * heads of 0 is a no-op, with these exceptions: plora_kv_plan still writes its
+ * per-request outputs, and plora_rope_append with heads of 0 has no q to turn but
+ * stores k and v (with kv_heads of 0 it turns q alone).
  * What only the device can see never faults: a request that cannot be served is
  * left out and counted, a slot or page id outside the pool is not written and
  * reads as zeros.
@@ -138,7 +140,8 @@ plora_status plora_rope(const void* x, int64_t x_token, int64_t x_head, const in
 /*
  * q rotated into q_out (which may be q itself), k rotated into the cache and v
  * copied there, token t at slot[t]; a token whose slot is negative or outside
- * the pool is not stored (its q is rotated all the same).  cache gives the
+ * the pool is not stored (its q is rotated all the same).  Either may be absent:
+ * heads of 0 (q and q_out NULL) or kv_heads of 0 (k and v NULL).  cache gives the
  * key heads, the head dimension and the type of all four.  slots of one call
  * must differ.
  */
