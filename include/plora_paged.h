@@ -193,7 +193,7 @@ size_t plora_attn_paged_workspace_bytes(const plora_attn_shape* shape);
  * request shares if its new tokens lie behind the prefix, it has at most
  * PLORA_ATTN_SHARE_ROWS query rows per key head (one with more fills the matrix
  * units by itself), and another request of its group does.  Without groups seg
- * and prefix_len are NULL.  One launch.
+ * and prefix_len are NULL; with n_groups of 0 prefix_len may be.  One launch.
  *
  * int32 word PLORA_ATTN_PLAN_LEFT_OUT of the plan is the number of requests that
  * have tokens in the step and are left out here, their outputs zeros: those of

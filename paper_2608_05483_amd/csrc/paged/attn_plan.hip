@@ -433,7 +433,7 @@ extern "C" plora_status plora_attn_plan(const plora_kv_step* step, const plora_a
   if (!shape_ok(*shape) || !page_size_ok(step->page_size)) return PLORA_ERR_UNSUPPORTED;
   if (shape_empty(*shape)) return PLORA_OK;
   if (!step->q_start || !step->kv_len || !step->req || !plan) return PLORA_ERR_INVALID_ARG;
-  if (seg && (!prefix_len || !seg->perm || !seg->seg_ptr || !seg->seg_id || !seg->meta ||
+  if (seg && ((n_groups > 0 && !prefix_len) || !seg->perm || !seg->seg_ptr || !seg->seg_id || !seg->meta ||
               seg->cap != std::min(seg->T, n_groups)))
     return PLORA_ERR_INVALID_ARG;
   if (!aligned(plan, 16)) return PLORA_ERR_UNSUPPORTED;

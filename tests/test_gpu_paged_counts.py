@@ -64,3 +64,12 @@ def test_requests_of_no_tokens_behind_too_many(G, P):
         assert (got["kv_len"] == 16).all() and (got["req"] == -1).all()
         assert list(got["q_start"]) == [0, 0] + [20] * (n - 1)
         check_plan(G, past, new, np.arange(9), 0, np.zeros((n, 4), int), 16, 20)
+
+
+def test_no_groups_yet(G, P):
+    """A batch grouped over no groups at all: every request by itself."""
+    b = Batch(G, P, [10, 300, 0], [1, 1, 4], 4, 2, group=np.full(3, -1), prefix=[0])
+    segs = P.Segments(3, 0)
+    P.segment(i32([-1] * 3), segs)
+    G.attn_plan(b.step, b.plan, segs, i32([]))
+    check(b.run(0.2), *b.ref(0.2), BF, 320)
