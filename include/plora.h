@@ -417,8 +417,8 @@ plora_status plora_workspace_counters(const void* ws, size_t ws_bytes, int64_t* 
 /* Static string naming a status code. */
 const char* plora_status_string(plora_status status);
 
-/* Test hook: the hipError_t of the most recent launch that returned
- * PLORA_ERR_HIP in this process, 0 if none did. */
+/* Test hook: the hipError_t of the most recent launch of this header's calls
+ * that returned PLORA_ERR_HIP in this process, 0 if none did. */
 int32_t plora_debug_last_hip_error(void);
 
 /* Test hook: how many times a one-launch plora_apply work item re-reads a

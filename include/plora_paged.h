@@ -227,6 +227,10 @@ plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t q_head,
                               size_t plan_bytes, void* out, int64_t out_token, int64_t out_head,
                               void* ws, size_t ws_bytes, hipStream_t stream);
 
+/* Test hook: the hipError_t of the most recent launch of this header's calls
+ * that returned PLORA_ERR_HIP in this process, 0 if none did. */
+int32_t plora_paged_last_hip_error(void);
+
 #ifdef __cplusplus
 }
 #endif

@@ -174,6 +174,8 @@ __global__ __launch_bounds__(kNT) void kv_plan_kernel(
 }  // namespace
 }  // namespace paged
 
+extern "C" int32_t plora_paged_last_hip_error(void) { return paged::g_last_hip_error.load(); }
+
 extern "C" plora_status plora_kv_plan(const int32_t* past, const int32_t* n_new,
                                       const int32_t* free_pages, int32_t n_free,
                                       const int32_t* free_head, int32_t* free_next,

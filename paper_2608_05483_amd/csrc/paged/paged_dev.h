@@ -4,6 +4,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <cstddef>
 #include <cstdint>
 
@@ -100,10 +101,14 @@ inline int32_t log2_of(int32_t v) {
 }
 
 // The status of the launch just made (an error left by earlier HIP calls is
-// cleared before it by clear_error).
+// cleared before it by clear_error), its error kept for plora_paged_last_hip_error.
+inline std::atomic<int32_t> g_last_hip_error{0};
 inline void clear_error() { (void)hipGetLastError(); }
 inline plora_status launch_status() {
-  return hipGetLastError() == hipSuccess ? PLORA_OK : PLORA_ERR_HIP;
+  const hipError_t e = hipGetLastError();
+  if (e == hipSuccess) return PLORA_OK;
+  g_last_hip_error.store((int32_t)e);
+  return PLORA_ERR_HIP;
 }
 
 }  // namespace paged

@@ -31,7 +31,8 @@ SHARE_ROWS = 128
 PLAN_LEFT_OUT = 6
 
 EXPORTED = ("plora_kv_plan", "plora_rope", "plora_rope_append", "plora_attn_plan_bytes",
-            "plora_attn_paged_workspace_bytes", "plora_attn_plan", "plora_attn_paged")
+            "plora_attn_paged_workspace_bytes", "plora_attn_plan", "plora_attn_paged",
+            "plora_paged_last_hip_error")
 
 
 class plora_kv_cache(ctypes.Structure):
@@ -76,6 +77,8 @@ def _declare(L) -> None:
     for fn in ("plora_attn_plan_bytes", "plora_attn_paged_workspace_bytes"):
         getattr(L, fn).argtypes = [SH]
         getattr(L, fn).restype = sz
+    L.plora_paged_last_hip_error.argtypes = []
+    L.plora_paged_last_hip_error.restype = i32
 
 
 _declare(lib)
@@ -101,7 +104,7 @@ def _stream(stream, dev: int) -> int:
 
 def _ok(fn: str, status: int) -> None:
     if status != PLORA_OK:
-        raise PloraError(fn, status)
+        raise PloraError(fn, status, lib.plora_paged_last_hip_error)
 
 
 def _dtype(t) -> int:

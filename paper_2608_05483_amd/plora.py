@@ -50,10 +50,12 @@ EXPORTED = ("plora_tile_capacity", "plora_workspace_bytes", "plora_workspace_ini
 
 
 class PloraError(RuntimeError):
-    def __init__(self, fn: str, status: int):
+    def __init__(self, fn: str, status: int, hip_error=None):
+        """hip_error: the hook that names a failed launch's error, if it is not
+        plora_debug_last_hip_error."""
         msg = f"{fn}: {status_string(status)}"
         if status == PLORA_ERR_HIP:
-            msg += f" (hipError_t {int(lib.plora_debug_last_hip_error())})"
+            msg += f" (hipError_t {int((hip_error or lib.plora_debug_last_hip_error)())})"
         super().__init__(msg)
         self.status = status
 

@@ -385,3 +385,16 @@ def test_the_plan_s_count_is_where_the_header_says():
 def test_oracle_keeps_requests_of_no_tokens():
     r = OP.kv_plan([16, 16, 16], [0, 30, 0], [1, 2, 3], 0, np.zeros((3, 4), int), 16, 20)
     assert r["meta"][:3] == [20, 0, 1] and r["kv_len"] == [16, 16, 16]
+
+
+def test_a_failed_launch_names_its_error():
+    """Where there is no GPU, a launch fails with the runtime's "no device"."""
+    import torch
+    if torch.cuda.device_count():
+        pytest.skip("launches succeed here")
+    assert plan_status() == P.PLORA_ERR_HIP
+    assert P.lib.plora_paged_last_hip_error() == 100
+    assert attn_plan_status() == rope_status() == append_status() == attn_status() == \
+        P.PLORA_ERR_HIP
+    with pytest.raises(P.PloraError, match="hipError_t 100"):
+        G._ok("plora_rope", rope_status())
