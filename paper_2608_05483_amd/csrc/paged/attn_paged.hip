@@ -440,17 +440,18 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
 // through registers into LDS and V transposed there 2.4 us; with a maximum each step
 // and a sum by additions 2.7; eight wavefronts a work group in two phases, one
 // side's products beside the other's exponentials, 2.8.
-// Schedules n products, each fed by r reads from LDS, four products' reads ahead.
-template <int N, int R>
+// Schedules n times P products, each time fed by r reads from LDS, four times' reads
+// ahead.
+template <int N, int R, int P = 1>
 __device__ __forceinline__ void feed() {
   constexpr int kAhead = 4;
   __builtin_amdgcn_sched_group_barrier(0x100, R * kAhead, 0);
 #pragma unroll
   for (int i = 0; i < N - kAhead; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, P, 0);
     __builtin_amdgcn_sched_group_barrier(0x100, R, 0);
   }
-  __builtin_amdgcn_sched_group_barrier(0x008, kAhead, 0);
+  __builtin_amdgcn_sched_group_barrier(0x008, P * kAhead, 0);
 }
 
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -466,7 +467,7 @@ __device__ __forceinline__ u32x2 read_columns(const uint16_t* p) {
 // Waits for this wavefront's loads (those into LDS among them).
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
-template <class Ty, int D>
+template <class Ty, int D, bool TWO>
 __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int kvh,
                                           int* s_most, u32x4* s_k0, u32x4* s_k1, u32x4* s_v0,
                                           u32x4* s_v1) {
@@ -593,7 +594,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
           for (int i = 0; i < 16; ++i)
             s[b][i] = 32 * b + 8 * (i >> 2) + (i & 3) < lim ? s[b][i] : -INFINITY;
       }
-      u32x4 p[4];
+      u32x4 p[4], rest[TWO ? 4 : 1];
       const auto weights = [&]() {
         const float ms = (m == -INFINITY ? 0.f : m) - Ty::kTileLift;
         float sum0 = 0.f, sum1 = 0.f;
@@ -601,11 +602,17 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
         for (int b = 0; b < 2; ++b)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            const uint32_t w = Ty::pack(exp2_(fmaf(s[b][2 * i], a.c, -ms)),
-                                        exp2_(fmaf(s[b][2 * i + 1], a.c, -ms)));
+            const float p0 = exp2_(fmaf(s[b][2 * i], a.c, -ms)),
+                        p1 = exp2_(fmaf(s[b][2 * i + 1], a.c, -ms));
+            const uint32_t w = Ty::pack(p0, p1);
             p[2 * b + (i >> 2)][i & 3] = w;
-            if (i & 1) sum1 = Ty::sum2(w, sum1);
-            else sum0 = Ty::sum2(w, sum0);
+            if constexpr (TWO) {
+              rest[2 * b + (i >> 2)][i & 3] = Ty::pack(p0 - Ty::lo(w), p1 - Ty::hi(w));
+              sum0 += p0, sum1 += p1;
+            } else {
+              if (i & 1) sum1 = Ty::sum2(w, sum1);
+              else sum0 = Ty::sum2(w, sum0);
+            }
           }
         return sum0 + sum1;
       };
@@ -636,9 +643,11 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
         for (int d = 0; d < kV; ++d) {
           const uint16_t* v = vp + 16 * b * D + ((32 * d) ^ (turn_v(vrow) * 8));
           const u32x2 v0 = read_columns(v), v1 = read_columns(v + 8 * D);
-          acc[d] = mfma32(Ty{}, u32x4{v0[0], v0[1], v1[0], v1[1]}, p[b], acc[d]);
+          const u32x4 vt = {v0[0], v0[1], v1[0], v1[1]};
+          acc[d] = mfma32(Ty{}, vt, p[b], acc[d]);
+          if constexpr (TWO) acc[d] = mfma32(Ty{}, vt, rest[b], acc[d]);
         }
-      feed<4 * kV, 2>();
+      feed<4 * kV, 2, TWO ? 2 : 1>();
       __builtin_amdgcn_sched_barrier(0);
     }
     loads_done();
@@ -694,7 +703,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 // are a multiple of 8.
 constexpr uint32_t kRun = 32;
 template <class Ty, int D, int POL>
-__global__ __launch_bounds__(kNT, 2) void items_kernel(AttnArgs a) {
+__global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a) {
   // (buffers by name: reads of one are seen not to meet the loads into the other)
   __shared__ u32x4 s_k0[kTileStep * D / 8], s_k1[kTileStep * D / 8];
   __shared__ u32x4 s_v0[kTileStep * D / 8], s_v1[kTileStep * D / 8];
@@ -716,8 +725,10 @@ __global__ __launch_bounds__(kNT, 2) void items_kernel(AttnArgs a) {
   if (item >= (uint32_t)(tile ? a.head->tiles : all_few)) return;
   const Item it = tile ? a.tile[item]
                        : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
-  if (tile)
-    tile_item<Ty, D>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
+  if (tile && it.gathered)
+    tile_item<Ty, D, true>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
+  else if (tile)
+    tile_item<Ty, D, false>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
   else
     few_item<Ty, D, POL, true>(a, it, kvh, sh, reinterpret_cast<f32x4*>(s_k0),
                                reinterpret_cast<f32x4*>(s_k1));
