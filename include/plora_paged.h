@@ -216,10 +216,13 @@ plora_status plora_attn_plan(const plora_kv_step* step, const plora_attn_shape* 
  * 8), pointers 16-byte aligned, cache strides multiples of 8, the token stride
  * from head_dim to below 2^25 (a pool may have its pages, heads and keys in any
  * order).  Scores, weights and sums are fp32; the weights enter the product with
- * v as two values of the type (16 bits) where a tile has up to 16 rows, as one
- * above, where that product bounds the call.  plan: as plora_attn_plan wrote it
- * for the same step and shape; ws: at least plora_attn_paged_workspace_bytes
- * bytes, 16-byte aligned, no contents needed.
+ * v as two values of the type (bf16: 16 bits) for requests of up to 16 query rows
+ * per key head, and for others over a prefix that they share; as one (bf16: 8
+ * bits) over the own keys of a request of more rows, where that product bounds
+ * the call.  So a request's own size says how its weights are rounded, and the
+ * batch that it is in never rounds them more.  out must not overlap q.  plan: as
+ * plora_attn_plan wrote it for the same step and shape; ws: at least
+ * plora_attn_paged_workspace_bytes bytes, 16-byte aligned, no contents needed.
  */
 plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t q_head,
                               const plora_kv_cache* cache, const plora_kv_step* step,

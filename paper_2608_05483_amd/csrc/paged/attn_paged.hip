@@ -428,10 +428,15 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
 // whether that still stands: it is only raised, the output rescaled and the weights
 // formed again, if a lane's sum of 32 passes kBar (bf16 2^13; fp16 2^16, above which
 // a weight becomes infinite and the sum with it).  So no maximum is looked for in
-// most steps, and no weight is more than its type holds.  The weights are summed as
-// rounded to the type, which they are for the product with V: its rounding errors
-// average out below the output's own, and a second product for the rest would add
-// half to the work that bounds the kernel.
+// most steps, and no weight is more than its type holds.
+// A request's own keys (more than 16 rows): the weights enter the product with V as
+// one value of the type and are summed as rounded so.  A second product for the rest
+// would add half to the work that bounds the kernel (5 prompts of 1500..5000 tokens x
+// 32 heads: 600 us, 815 with it; 32 of 1..512 x 64, fp16: 371, 498); with one, the
+// output is off by 1.4 times its own rounding (2.3e-3 of its norm in bf16, 1.66e-3 with
+// two).  TWO, for a prefix that requests share: two values, as in a few item, so that
+// a request's weights do not count to fewer bits for the company that it is in (256
+// requests in 6 groups x 64 heads over 8, both kernels: 180 us, 175 with one).
 // Bound by the matrix units and what they cannot hide: for 64 keys and 32 rows 32
 // products (1024 cycles), 64 vector instructions and 32 exponentials (512), 64 reads
 // of LDS (about 600).  64 keys x 128 rows, two work groups on every compute unit:
@@ -701,6 +706,8 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 // 3 groups x 40 heads: 93, 96, 99, 102).  Eight work groups in a row are of one kind,
 // so that a head's items, which share K and V, stay on one XCD where the key heads
 // are a multiple of 8.
+// (Two work groups on a compute unit at D 128, three at 64, to which the fp16 form is
+// held: 5 registers spilt; prompts of 1500..5000 tokens: 351 us, 367 with two.)
 constexpr uint32_t kRun = 32;
 template <class Ty, int D, int POL>
 __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a) {
