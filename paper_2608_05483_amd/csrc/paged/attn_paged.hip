@@ -87,19 +87,18 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc(const uint16_t* x, const 
                                            kRsrcWord3);
 }
 
-// POL: the cache policy.
-constexpr int kCached = 0, kOnce = 2;      // default, non-temporal
-template <int POL>
+// The few items' loads of K and V, which each reads once: non-temporal.  Layers in
+// turn, both kernels, so and by the default policy: one request of 30011 keys on 8
+// heads, 8 layers of 123 MB, 30.8 us a layer and 32.5; 16 of 1001 keys, 8 of 67 MB, 19.6
+// and 22.5; 64 of 501, 8 of 135 MB, 27.1 and 30.9.  Only where all layers stay in the
+// last-level cache is the default faster: one request of 3001 keys, 16 layers of 13 MB,
+// 16.0 and 15.1 (32 of them, 16.0 and 17.0).
+constexpr int kOnce = 2;
 __device__ __forceinline__ u32x4 bld16(__amdgpu_buffer_rsrc_t r, int off) {
-  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, POL));
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, kOnce));
 }
-template <int POL>
 __device__ __forceinline__ u32x2 bld8(__amdgpu_buffer_rsrc_t r, int off) {
-  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, POL));
-}
-template <int POL>
-__device__ __forceinline__ uint32_t bld4(__amdgpu_buffer_rsrc_t r, int off) {
-  return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, POL);
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, kOnce));
 }
 
 // Words of 16-bit pairs (a's, b's) of the low or high halves.
@@ -217,7 +216,7 @@ struct FewShared {
   float m[kWaves][kFew], l[kWaves][kFew];
   int bad, most[kWaves];
 };
-template <class Ty, int D, int POL, bool AHEAD>
+template <class Ty, int D, bool AHEAD>
 __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int kvh,
                                          FewShared& sh, f32x4* o01, f32x4* o23) {
   constexpr int kQ = D / 32;             // 16-byte units of a row, per lane
@@ -246,7 +245,7 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
       const auto rk = rsrc(a.k, cell[b]);
 #pragma unroll
       for (int j = 0; j < kQ; ++j)
-        x.k[b][j] = bld16<POL>(rk, (n * a.key_stride + 32 * j + 8 * g) * 2);
+        x.k[b][j] = bld16(rk, (n * a.key_stride + 32 * j + 8 * g) * 2);
     }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -255,11 +254,11 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
       for (int i = 0; i < 4; ++i) {
         const int off = ((4 * g + i) * a.key_stride + kV * n) * 2;
         if constexpr (kV == 8) {
-          const u32x4 w = bld16<POL>(rv, off);
+          const u32x4 w = bld16(rv, off);
 #pragma unroll
           for (int e = 0; e < 4; ++e) x.v[4 * b + i][e] = w[e];
         } else {
-          const u32x2 w = bld8<POL>(rv, off);
+          const u32x2 w = bld8(rv, off);
 #pragma unroll
           for (int e = 0; e < 2; ++e) x.v[4 * b + i][e] = w[e];
         }
@@ -406,7 +405,7 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
 }
 
 // The few items of a step that can have no others.
-template <class Ty, int D, int POL>
+template <class Ty, int D>
 __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
   __shared__ f32x4 o01[2 * kFew * D / 4], o23[2 * kFew * D / 4];
   __shared__ FewShared sh;
@@ -414,7 +413,7 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
   const int item = blockIdx.x / a.kv_heads, first = a.head->few;
   if (item >= first + a.head->later) return;
   const Item it = item < first ? a.few[item] : a.last_few[first - item];
-  few_item<Ty, D, POL, false>(a, it, blockIdx.x % a.kv_heads, sh, o01, o23);
+  few_item<Ty, D, false>(a, it, blockIdx.x % a.kv_heads, sh, o01, o23);
 }
 
 // Items of up to 128 rows: prompts, and prefixes that many rows share.  A wavefront
@@ -709,7 +708,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 // (Two work groups on a compute unit at D 128, three at 64, to which the fp16 form is
 // held: 5 registers spilt; prompts of 1500..5000 tokens: 351 us, 367 with two.)
 constexpr uint32_t kRun = 32;
-template <class Ty, int D, int POL>
+template <class Ty, int D>
 __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a) {
   // (buffers by name: reads of one are seen not to meet the loads into the other)
   __shared__ u32x4 s_k0[kTileStep * D / 8], s_k1[kTileStep * D / 8];
@@ -737,8 +736,8 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   else if (tile)
     tile_item<Ty, D, false>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
   else
-    few_item<Ty, D, POL, true>(a, it, kvh, sh, reinterpret_cast<f32x4*>(s_k0),
-                               reinterpret_cast<f32x4*>(s_k1));
+    few_item<Ty, D, true>(a, it, kvh, sh, reinterpret_cast<f32x4*>(s_k0),
+                          reinterpret_cast<f32x4*>(s_k1));
 }
 
 // Joins a row's partials: its request's own pieces, then its prefix's.  D / 4 lanes
@@ -896,13 +895,6 @@ WsLayout ws_layout(const plora_attn_shape& s, const Bounds& b) {
   return w;
 }
 
-// Whether K and V are read with the default cache policy, so that a small cache
-// may still be in the last-level cache in the next step, or non-temporally: by the
-// size of the pool, as the host does not know the lengths (one request of 30011
-// keys on 8 heads, 123 MB: 22.6 us by default, 24.8 non-temporally; 64 x 32 x
-// 512..4096, 2.4 GB: 435 and 404; 256 requests, 0.6 GB: 128 and 124).
-constexpr int64_t kKeep = INT64_C(192) << 20;
-
 // Work groups for the caps of both kinds, in eights.
 int64_t item_blocks(const Bounds& b, int32_t kv_heads) {
   const int64_t few = (int64_t)b.few_cap * kv_heads, tiles = (int64_t)b.tile_cap * kv_heads;
@@ -910,15 +902,14 @@ int64_t item_blocks(const Bounds& b, int32_t kv_heads) {
 }
 
 template <class Ty, int D>
-plora_status launch(const AttnArgs& a, const Bounds& b, int64_t pool_bytes, hipStream_t stream) {
-  const bool keep = pool_bytes <= kKeep;
+plora_status launch(const AttnArgs& a, const Bounds& b, hipStream_t stream) {
   clear_error();
   if (b.tile_cap > 0)
-    hipLaunchKernelGGL((keep ? items_kernel<Ty, D, kCached> : items_kernel<Ty, D, kOnce>),
-                       dim3(item_blocks(b, a.kv_heads)), dim3(kNT), 0, stream, a);
+    hipLaunchKernelGGL((items_kernel<Ty, D>), dim3(item_blocks(b, a.kv_heads)), dim3(kNT), 0,
+                       stream, a);
   else
-    hipLaunchKernelGGL((keep ? few_kernel<Ty, D, kCached> : few_kernel<Ty, D, kOnce>),
-                       dim3(b.few_cap * a.kv_heads), dim3(kNT), 0, stream, a);
+    hipLaunchKernelGGL((few_kernel<Ty, D>), dim3(b.few_cap * a.kv_heads), dim3(kNT), 0, stream,
+                       a);
   plora_status st = launch_status();
   if (st != PLORA_OK) return st;
   // Few rows: a work group for what otherwise is a wavefront's.  Else heads of a
@@ -1018,10 +1009,7 @@ extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t
   a.pm = reinterpret_cast<float*>(wp);
   a.pl = reinterpret_cast<float*>(wp + w.l);
   a.po = reinterpret_cast<float*>(wp + w.o);
-  const int64_t pool = (int64_t)c.n_pages * c.page_size * s.kv_heads * s.head_dim * 4;
   if (c.dtype == PLORA_BF16)
-    return s.head_dim == 128 ? launch<Bf16, 128>(a, b, pool, stream)
-                             : launch<Bf16, 64>(a, b, pool, stream);
-  return s.head_dim == 128 ? launch<Fp16, 128>(a, b, pool, stream)
-                           : launch<Fp16, 64>(a, b, pool, stream);
+    return s.head_dim == 128 ? launch<Bf16, 128>(a, b, stream) : launch<Bf16, 64>(a, b, stream);
+  return s.head_dim == 128 ? launch<Fp16, 128>(a, b, stream) : launch<Fp16, 64>(a, b, stream);
 }
