@@ -671,7 +671,10 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
   for (int d = 0; d < kV; ++d)
 #pragma unroll
     for (int i = 0; i < 16; ++i) fine = fine && fabsf(acc[d][i]) < INFINITY;
-  if (mine) {
+  // (a row's two lanes agree on it; careful_row's lanes, which are others, write it then)
+  uint64_t bad = __ballot(mine && !fine);
+  bad = (bad | bad >> 32) & 0xffffffffu;
+  if (mine && !(bad >> n & 1)) {
     const float inv = any ? 1.f / l : 0.f;
     const int64_t at = ((int64_t)it.part + 32 * wv + n) * a.kv_heads + kvh;
     if (it.part >= 0 && h == 0) a.pm[at] = m - Ty::kTileLift, a.pl[at] = l;
@@ -687,8 +690,6 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
           store_part<4>(a.po + at * D + e, o);
       }
   }
-  uint64_t bad = __ballot(mine && !fine);
-  bad = (bad | bad >> 32) & 0xffffffffu;
   while (bad) {
     const int i = __builtin_ctzll(bad);
     bad &= bad - 1;
