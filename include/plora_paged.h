@@ -105,10 +105,12 @@ typedef struct {
  * ceil(past_b / page_size) of them, into the entries of its row that follow the
  * held ones.  *free_next = *free_head + the pages taken.  Inputs and outputs
  * must not overlap (a loop hands kv_len and free_next to the next step as past
- * and free_head).  A request is left out if past or n_new is negative, its
- * length passes max_pages page_size, its tokens pass T, or the free list is too
- * short for it (then every later request that needs a page is left out too):
- * it takes no pages, its kv_len is max(past, 0), its tokens are padding.
+ * and free_head).  The pages of a request that has ended are the caller's to put
+ * behind the list's end or into a later step's list.  A request is left out if
+ * past or n_new is negative, its length passes max_pages page_size, its tokens
+ * pass T, or the free list is too short for it (then every later request that
+ * needs a page is left out too): it takes no pages, its kv_len is max(past, 0),
+ * its tokens are padding.
  * Requests of n_new 0 keep their length.  One launch.
  */
 plora_status plora_kv_plan(const int32_t* past, const int32_t* n_new,

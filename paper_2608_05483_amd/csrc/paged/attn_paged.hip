@@ -701,11 +701,11 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 // matrix units.  They come in turn, kRun eights of each until one kind is used up:
 // a run is a work group for every compute unit, and each holds two, so that a tile
 // item has one of another kind beside it, and the long tile items have begun early.
-// Both calls of a layer, 256 requests in 6 groups: 163 us; in turn by each eight 176,
-// spread in proportion over the launch 193, all tile items first 163 (45 requests in
-// 3 groups x 40 heads: 93, 96, 99, 102).  Eight work groups in a row are of one kind,
-// so that a head's items, which share K and V, stay on one XCD where the key heads
-// are a multiple of 8.
+// Both kernels, 256 requests in 6 groups: 179 us; in turn by each eight 202.  (With
+// weights of one value over the prefixes 163; spread in proportion over the launch 193,
+// all tile items first 163; a layer of 45 requests in 3 groups x 40 heads 93, 99, 102.)
+// Eight work groups in a row are of one kind, so that a head's items, which share K and
+// V, stay on one XCD where the key heads are a multiple of 8.
 // (Two work groups on a compute unit at D 128, three at 64, to which the fp16 form is
 // held: 5 registers spilt; prompts of 1500..5000 tokens: 351 us, 367 with two.)
 constexpr uint32_t kRun = 32;
@@ -746,7 +746,7 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
 // D / 4 pieces are found at once, a lane a piece, then eight partials are asked for
 // at a time.  WIDE: four wavefronts for the same rows, a quarter of the pieces each,
 // joined in a fixed order (few rows, cut into many pieces: one request of 30011 keys
-// x 64 heads, 59 pieces: 10.0 us with a wavefront a row, 5.4 so).  Rows that the
+// x 64 heads, 59 pieces: 10.0 us with a wavefront a row, about 5 so).  Rows that the
 // items wrote themselves are left, rows without a key get zeros.  Bound by reading
 // the partials, or by the latency of its chain of loads.
 template <class Ty, int D, bool WIDE>

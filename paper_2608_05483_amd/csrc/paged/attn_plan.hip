@@ -127,15 +127,17 @@ __device__ __forceinline__ void emit(const PlanArgs& a, const Set& x, int j, int
 // ones cost little (64 requests x 32 heads x 512..4096 keys: 402 us at 768, 392 at
 // 2048, 380 at 4096), and pieces of less than 512 keys pay more for their start and
 // their partials than they gain (one request of 30011 keys on 8 heads, both
-// kernels: 42 us at 256, 33 at 512).  Sets of at most half of that come last, so that
+// kernels: 32 us at 256, 28 at 512).  Sets of at most half of that come last, so that
 // what is begun last is short (256 requests of 33..543 keys on 8 heads: 67 us in the
 // requests' order, 63 so; 180 of 9..708 on 40: 230 and 223).
 // Tile items: the number of pieces changes how many rounds the chip's kTileSlots
-// work groups (two per compute unit) take, so several cuts are tried, a wavefront
-// each, and the one whose rounds x (longest piece + kTileStart) is least is taken
-// (256 requests in 6 groups x 64 heads over 8, prefixes of 4000 keys: 608 work
-// groups, two rounds, 81 us; 456, one, 64; the tile items alone).  kTileStart is what
-// a piece costs beside its keys, most of it the writing and reading of its partials.
+// work groups (two per compute unit, at a head dimension of 128; at 64 three fit, for
+// which the rounds are then counted too many) take, so several cuts are tried, a
+// wavefront each, and the one whose rounds x (longest piece + kTileStart) is least is
+// taken (256 requests in 6 groups x 64 heads over 8, prefixes of 4000 keys: 608 work
+// groups, two rounds, 81 us; 456, one, 64; the tile items alone, with weights of one
+// value).  kTileStart is what a piece costs beside its keys, most of it the writing and
+// reading of its partials.
 //
 // Once a step and bound by latency: dependent loads, barriers, and code that is
 // fetched for the first time.
