@@ -178,6 +178,8 @@ class Step:
         self.q_start = torch.zeros(batch + 1, **i32)
         self.dev = self.q_start.get_device()
         _ints("table", self.table, _I32, batch * max_pages, self.dev)
+        if self.table.dim() > 1 and tuple(self.table.shape[1:]) != (max_pages,):
+            raise ValueError("table: rows of max_pages entries expected")
         self.kv_len = torch.zeros(batch, **i32)
         self.pos = torch.zeros(T, **i32)
         self.req = torch.full((T,), -1, **i32)

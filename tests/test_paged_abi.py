@@ -398,3 +398,15 @@ def test_a_failed_launch_names_its_error():
         P.PLORA_ERR_HIP
     with pytest.raises(P.PloraError, match="hipError_t 100"):
         G._ok("plora_rope", rope_status())
+
+
+def test_a_table_of_other_rows_is_refused():
+    """Rows of another length than max_pages would be read as each other's pages; more
+    rows than requests, or a flat table, are fine."""
+    import torch
+    t = lambda *s: torch.zeros(s, dtype=torch.int32)
+    for bad in (t(3, 6), t(4, 4), t(3, 4), t(2, 5), t(3, 10)[:, :5], t(3, 5, 2)):
+        with pytest.raises(ValueError):
+            G.Step(3, 4, 16, 5, device="cpu", table=bad)
+    for good in (t(3, 5), t(9, 5), t(15)):
+        assert G.Step(3, 4, 16, 5, device="cpu", table=good).table is good
