@@ -9,10 +9,17 @@
 // dimension, eight keys in a lane: few_kernel loads eight rows and transposes the
 // 16-bit block in the lane's own registers, tile_kernel reads columns from LDS.
 // The scores are kept times scale log2(e), so a weight is one exp2 of one fma.
+//
+// TREE (include/plora_tree.h, plora_attn_tree): a row sees, of its request's new keys,
+// those whose interval of preorder numbers holds the row's own number.  A node's
+// ancestors have lower numbers than it, so a row's last key is the one that it has
+// without a tree, and the plan is the same; only in the steps that reach new keys does
+// a lane compare the intervals of its keys.
 
 #include <cmath>
 
 #include "attn_plan.h"
+#include "plora_tree.h"
 
 namespace paged {
 namespace {
@@ -35,6 +42,7 @@ struct AttnArgs {
   uint32_t flip;            // sign bits for q where scale < 0
   uint16_t* out;
   float *pm, *pl, *po;      // partials: [row][kv_heads], [row][kv_heads][D]
+  const int2 *span, *tree;  // trees: intervals by token, kinds by request
 };
 
 __device__ __forceinline__ f32x4 mfma16(Bf16, u32x4 a, u32x4 b, f32x4 c) {
@@ -106,19 +114,50 @@ __device__ __forceinline__ uint32_t zip(uint32_t a, uint32_t b, bool high) {
   return high ? __builtin_amdgcn_perm(b, a, 0x07060302u) : __builtin_amdgcn_perm(b, a, 0x05040100u);
 }
 
-// A query row: its token, its head, the keys it sees.
+// A query row: its token, its head, the end of the keys it sees, its preorder number.
 struct Row {
-  int token, head, limit;
+  int token, head, limit, number;
 };
+template <bool TREE>
 __device__ __forceinline__ Row query_row(const AttnArgs& a, const Item& it, int kvh, int i) {
-  Row x{0, 0, it.lo};
+  Row x{0, 0, it.lo, -1};
   if (i < it.rows) {
     const int R = it.row + i, tk = it.tok + R / a.r;
     x.token = it.gathered ? a.order[tk] : tk;
     x.head = kvh * a.r + R % a.r;
     x.limit = max(it.lo, min(it.hi, a.pos[x.token] + 1));
+    if constexpr (TREE) {
+      x.number = a.span[x.token].x;
+      if (x.number < 0) x.limit = it.lo;
+    }
   }
   return x;
+}
+
+// Where an item's keys are the new ones of a tree: from key past on, key j is that of
+// token j - shift.  (Chains and prefixes have none.)
+struct NewKeys {
+  int past, shift;
+};
+template <bool TREE>
+__device__ __forceinline__ NewKeys new_keys(const AttnArgs& a, const Item& it) {
+  NewKeys x{INT32_MAX, 0};
+  if constexpr (TREE) {
+    if (!it.gathered && a.tree[it.req].x) {
+      x.past = a.pos[it.tok];
+      x.shift = x.past - it.tok;
+    }
+  }
+  return x;
+}
+// Whether a row sees a key below its limit.  (The token is one of the request's if the
+// step's arrays agree with each other, and one of the step's in any case.)
+template <bool TREE>
+__device__ __forceinline__ bool sees(const AttnArgs& a, const NewKeys& fresh, const Row& x,
+                                     int key) {
+  if (!TREE || key < fresh.past) return true;
+  const int2 s = a.span[min(max(key - fresh.shift, 0), a.T - 1)];
+  return s.x <= x.number && x.number <= s.y;
 }
 
 // One row by itself, in vector arithmetic over the keys it sees and no others,
@@ -127,18 +166,23 @@ __device__ __forceinline__ Row query_row(const AttnArgs& a, const Item& it, int 
 // they multiply the zero weight of a masked key with its value, which is not zero
 // if that value is an infinity or NaN.  Rare, and then the row's own infinities and
 // NaN come out as the sum gives them.
-template <class Ty, int D>
+template <class Ty, int D, bool TREE>
 __device__ __forceinline__ void careful_row(const AttnArgs& a, const Item& it, int kvh, int i) {
   constexpr int kPer = D / 64;
   const int lane = threadIdx.x & 63;
-  const Row x = query_row(a, it, kvh, i);
+  const Row x = query_row<TREE>(a, it, kvh, i);
+  const NewKeys fresh = new_keys<TREE>(a, it);
+  bool some = x.limit > it.lo && (!TREE || it.lo < fresh.past);
   const uint16_t* q = a.q + x.token * a.q_token + x.head * a.q_head;
   const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
   float m = -INFINITY, l = 0.f, acc[kPer] = {};
   for (int k0 = it.lo; k0 < x.limit; k0 += 64) {
     const int n = min(64, x.limit - k0);
     float s = -INFINITY;
-    if (lane < n) {
+    const bool seen = lane < n && sees<TREE>(a, fresh, x, k0 + lane);
+    const uint64_t all = TREE ? __ballot(seen) : 0;
+    some = some || all != 0;
+    if (seen) {
       const int key = k0 + lane, page = row[key >> a.log_page];
       s = 0.f;
       if (page >= 0 && page < a.n_pages) {
@@ -164,6 +208,7 @@ __device__ __forceinline__ void careful_row(const AttnArgs& a, const Item& it, i
     l = l * al + t;
     for (int j = 0; j < kPer; ++j) acc[j] *= al;
     for (int j = 0; j < n; ++j) {
+      if (TREE && !(all >> j & 1)) continue;
       const int key = k0 + j, page = uniform(row[key >> a.log_page]);
       const float w = __shfl(p, j, 64);
       if (page < 0 || page >= a.n_pages) continue;
@@ -172,11 +217,11 @@ __device__ __forceinline__ void careful_row(const AttnArgs& a, const Item& it, i
       for (int e = 0; e < kPer; ++e) acc[e] = fmaf(w, Ty::lo(vp[e]), acc[e]);
     }
   }
-  if (m == -INFINITY && x.limit > it.lo) l = NAN;     // every score -inf: 0 / 0
+  if (m == -INFINITY && some) l = NAN;                // every score -inf: 0 / 0
   if (it.part < 0) {
     uint16_t* o = a.out + x.token * a.out_token + x.head * a.out_head + kPer * lane;
     for (int e = 0; e < kPer; ++e)
-      o[e] = (uint16_t)Ty::pack(x.limit > it.lo ? acc[e] / l : 0.f, 0.f);
+      o[e] = (uint16_t)Ty::pack(some ? acc[e] / l : 0.f, 0.f);
   } else {
     const int64_t at = ((int64_t)it.part + i) * a.kv_heads + kvh;
     if (lane == 0) a.pm[at] = m, a.pl[at] = l;
@@ -212,11 +257,13 @@ __device__ __forceinline__ void store_part(float* po, const float (&o)[N]) {
 // (K as the 16x16x32 product's rows: key n of 16, 16-byte units; V as rows of eight
 // keys), and join through LDS at the end.  The weights enter the product with V as
 // two values, hi + lo, which costs nothing here and keeps them to 16 bits.
+// (most: of a tile item the last key of each wavefront's rows, of a few item with a
+// tree the rows that see any of the wavefront's keys)
 struct FewShared {
   float m[kWaves][kFew], l[kWaves][kFew];
   int bad, most[kWaves];
 };
-template <class Ty, int D, bool AHEAD>
+template <class Ty, int D, bool AHEAD, bool TREE>
 __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int kvh,
                                          FewShared& sh, f32x4* o01, f32x4* o23) {
   constexpr int kQ = D / 32;             // 16-byte units of a row, per lane
@@ -270,7 +317,9 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
   ask(k0);
   if (k0 < it.hi) load(ka, k0);
 
-  const Row x = query_row(a, it, kvh, n);
+  const Row x = query_row<TREE>(a, it, kvh, n);
+  const NewKeys fresh = new_keys<TREE>(a, it);
+  bool some = x.limit > it.lo && (!TREE || it.lo < fresh.past);
   u32x4 qf[kQ];
 #pragma unroll
   for (int j = 0; j < kQ; ++j) qf[j] = u32x4{0, 0, 0, 0};
@@ -279,7 +328,7 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
 #pragma unroll
     for (int j = 0; j < kQ; ++j) qf[j] = *reinterpret_cast<const u32x4*>(q + 32 * j) ^ a.flip;
   }
-  int least = n < it.rows ? x.limit : INT32_MAX;
+  int least = n < it.rows ? min(x.limit, fresh.past) : INT32_MAX;
 #pragma unroll
   for (int d = 1; d < 16; d <<= 1) least = min(least, __shfl_xor(least, d, 64));
   least = uniform(least);
@@ -302,8 +351,12 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
     for (int i = 0; i < 8; ++i) t[i] = s[i >> 2][i & 3] * a.c;
     if (k0 + 32 > least) {               // some row does not see all 32
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        t[i] = k0 + 16 * (i >> 2) + 4 * g + (i & 3) < x.limit ? t[i] : -INFINITY;
+      for (int i = 0; i < 8; ++i) {
+        const int key = k0 + 16 * (i >> 2) + 4 * g + (i & 3);
+        const bool seen = key < x.limit && sees<TREE>(a, fresh, x, key);
+        t[i] = seen ? t[i] : -INFINITY;
+        if constexpr (TREE) some = some || seen;
+      }
     }
     float mx = m;
 #pragma unroll
@@ -353,6 +406,12 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
   l += __shfl_xor(l, 16, 64);
   l += __shfl_xor(l, 32, 64);
   if (g == 0) sh.m[wv][n] = m, sh.l[wv][n] = l;
+  if constexpr (TREE) {
+    uint64_t w = __ballot(some);
+    w |= w >> 32;
+    w |= w >> 16;
+    if (lane == 0) sh.most[wv] = (int)w & 0xffff;
+  }
   // acc[d][i] is the output's dimension kV (4 g + i) + d of row n; in LDS the
   // 16-byte units of a row are turned by its number
   const auto place = [&](int w, int r, int unit) {
@@ -367,7 +426,7 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
   __syncthreads();
   const int i = tid >> 4, e = (tid & 15) * kV;
   if (i < it.rows) {
-    const Row y = query_row(a, it, kvh, i);
+    const Row y = query_row<TREE>(a, it, kvh, i);
     float M = sh.m[0][i];
 #pragma unroll
     for (int w = 1; w < kWaves; ++w) M = fmaxf(M, sh.m[w][i]);
@@ -384,7 +443,8 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
         for (int c = 0; c < 4; ++c) o[d + c] = fmaf(f, v[c], o[d + c]);
       }
     }
-    const bool any = y.limit > it.lo;
+    bool any = y.limit > it.lo;
+    if constexpr (TREE) any = (sh.most[0] | sh.most[1] | sh.most[2] | sh.most[3]) >> i & 1;
     if (M == -INFINITY && any) L = NAN;
     bool fine = true;
 #pragma unroll
@@ -401,11 +461,11 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
   }
   __syncthreads();
   for (int b = wv; b < it.rows; b += kWaves)
-    if (sh.bad >> b & 1) careful_row<Ty, D>(a, it, kvh, b);
+    if (sh.bad >> b & 1) careful_row<Ty, D, TREE>(a, it, kvh, b);
 }
 
 // The few items of a step that can have no others.
-template <class Ty, int D>
+template <class Ty, int D, bool TREE>
 __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
   __shared__ f32x4 o01[2 * kFew * D / 4], o23[2 * kFew * D / 4];
   __shared__ FewShared sh;
@@ -413,7 +473,7 @@ __global__ __launch_bounds__(kNT, 3) void few_kernel(AttnArgs a) {
   const int item = blockIdx.x / a.kv_heads, first = a.head->few;
   if (item >= first + a.head->later) return;
   const Item it = item < first ? a.few[item] : a.last_few[first - item];
-  few_item<Ty, D, false>(a, it, blockIdx.x % a.kv_heads, sh, o01, o23);
+  few_item<Ty, D, false, TREE>(a, it, blockIdx.x % a.kv_heads, sh, o01, o23);
 }
 
 // Items of up to 128 rows: prompts, and prefixes that many rows share.  A wavefront
@@ -471,7 +531,7 @@ __device__ __forceinline__ u32x2 read_columns(const uint16_t* p) {
 // Waits for this wavefront's loads (those into LDS among them).
 __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70); }
 
-template <class Ty, int D, bool TWO>
+template <class Ty, int D, bool TWO, bool TREE>
 __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int kvh,
                                           int* s_most, u32x4* s_k0, u32x4* s_k1, u32x4* s_v0,
                                           u32x4* s_v1) {
@@ -483,7 +543,9 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
   if (it.rows <= 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
-  const Row x = query_row(a, it, kvh, 32 * wv + n);
+  const Row x = query_row<TREE>(a, it, kvh, 32 * wv + n);
+  const NewKeys fresh = new_keys<TREE>(a, it);
+  bool any = x.limit > it.lo && (!TREE || it.lo < fresh.past);
   const bool mine = 32 * wv + n < it.rows;
   u32x4 qf[kQ];
 #pragma unroll
@@ -493,7 +555,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 #pragma unroll
     for (int j = 0; j < kQ; ++j) qf[j] = *reinterpret_cast<const u32x4*>(q + 16 * j) ^ a.flip;
   }
-  int most = x.limit, least = mine ? x.limit : INT32_MAX;
+  int most = x.limit, least = mine ? min(x.limit, fresh.past) : INT32_MAX;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
     most = max(most, __shfl_xor(most, d, 64));
@@ -597,6 +659,26 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 #pragma unroll
           for (int i = 0; i < 16; ++i)
             s[b][i] = 32 * b + 8 * (i >> 2) + (i & 3) < lim ? s[b][i] : -INFINITY;
+        if constexpr (TREE) {
+          if (k0 + kTileStep > fresh.past) {
+            // bit 16 b + i: whether s[b][i] is seen, four keys in a row at a time
+            uint32_t seen = 0;
+#pragma unroll 1
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                seen |= (uint32_t)(8 * j + e < lim && sees<TREE>(a, fresh, x, k0 + 4 * h + 8 * j + e))
+                        << (4 * j + e);
+            any = any || seen;
+#pragma unroll
+            for (int b = 0; b < 2; ++b)
+#pragma unroll
+              for (int i = 0; i < 16; ++i)
+                s[b][i] = seen >> (16 * b + i) & 1 ? s[b][i] : -INFINITY;
+          } else {
+            any = any || lim > 0;
+          }
+        }
       }
       u32x4 p[4], rest[TWO ? 4 : 1];
       const auto weights = [&]() {
@@ -663,7 +745,10 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
   }
   if (32 * wv >= it.rows) return;
   l += __shfl_xor(l, 32, 64);
-  const bool any = x.limit > it.lo;
+  if constexpr (TREE) {
+    const int other = __shfl_xor((int)any, 32, 64);   // (by all lanes)
+    any = any || other;
+  }
   if (m == -INFINITY && any) l = NAN;
   // acc[d][i] is the output's dimension 32 d + 8 (i / 4) + 4 h + i % 4 of row n
   bool fine = true;
@@ -693,7 +778,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
   while (bad) {
     const int i = __builtin_ctzll(bad);
     bad &= bad - 1;
-    careful_row<Ty, D>(a, it, kvh, 32 * wv + i);
+    careful_row<Ty, D, TREE>(a, it, kvh, 32 * wv + i);
   }
 }
 
@@ -709,7 +794,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 // (Two work groups on a compute unit at D 128, three at 64, to which the fp16 form is
 // held: 5 registers spilt; prompts of 1500..5000 tokens: 351 us, 367 with two.)
 constexpr uint32_t kRun = 32;
-template <class Ty, int D>
+template <class Ty, int D, bool TREE>
 __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a) {
   // (buffers by name: reads of one are seen not to meet the loads into the other)
   __shared__ u32x4 s_k0[kTileStep * D / 8], s_k1[kTileStep * D / 8];
@@ -733,11 +818,11 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   const Item it = tile ? a.tile[item]
                        : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
   if (tile && it.gathered)
-    tile_item<Ty, D, true>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
+    tile_item<Ty, D, true, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
   else if (tile)
-    tile_item<Ty, D, false>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
+    tile_item<Ty, D, false, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
   else
-    few_item<Ty, D, true>(a, it, kvh, sh, reinterpret_cast<f32x4*>(s_k0),
+    few_item<Ty, D, true, TREE>(a, it, kvh, sh, reinterpret_cast<f32x4*>(s_k0),
                           reinterpret_cast<f32x4*>(s_k1));
 }
 
@@ -902,14 +987,14 @@ int64_t item_blocks(const Bounds& b, int32_t kv_heads) {
   return ((few + 7) / 8 + (tiles + 7) / 8) * 8;
 }
 
-template <class Ty, int D>
+template <class Ty, int D, bool TREE>
 plora_status launch(const AttnArgs& a, const Bounds& b, hipStream_t stream) {
   clear_error();
   if (b.tile_cap > 0)
-    hipLaunchKernelGGL((items_kernel<Ty, D>), dim3(item_blocks(b, a.kv_heads)), dim3(kNT), 0,
+    hipLaunchKernelGGL((items_kernel<Ty, D, TREE>), dim3(item_blocks(b, a.kv_heads)), dim3(kNT), 0,
                        stream, a);
   else
-    hipLaunchKernelGGL((few_kernel<Ty, D>), dim3(b.few_cap * a.kv_heads), dim3(kNT), 0, stream,
+    hipLaunchKernelGGL((few_kernel<Ty, D, TREE>), dim3(b.few_cap * a.kv_heads), dim3(kNT), 0, stream,
                        a);
   plora_status st = launch_status();
   if (st != PLORA_OK) return st;
@@ -928,23 +1013,24 @@ plora_status launch(const AttnArgs& a, const Bounds& b, hipStream_t stream) {
   return launch_status();
 }
 
-}  // namespace
-}  // namespace paged
-
-extern "C" size_t plora_attn_paged_workspace_bytes(const plora_attn_shape* shape) {
-  using namespace paged;
-  if (!shape || !shape_ok(*shape) || shape_empty(*shape)) return 0;
-  return ws_layout(*shape, bounds(*shape)).bytes;
+template <bool TREE>
+plora_status run(const AttnArgs& a, const Bounds& b, int32_t head_dim, int32_t dtype,
+                 hipStream_t stream) {
+  if (dtype == PLORA_BF16)
+    return head_dim == 128 ? launch<Bf16, 128, TREE>(a, b, stream)
+                           : launch<Bf16, 64, TREE>(a, b, stream);
+  return head_dim == 128 ? launch<Fp16, 128, TREE>(a, b, stream)
+                         : launch<Fp16, 64, TREE>(a, b, stream);
 }
 
-extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t q_head,
-                                         const plora_kv_cache* cache, const plora_kv_step* step,
-                                         const plora_attn_shape* shape, float scale,
-                                         const void* plan, size_t plan_bytes, void* out,
-                                         int64_t out_token, int64_t out_head, void* ws,
-                                         size_t ws_bytes, hipStream_t stream) {
-  using namespace paged;
+// The checks of both entry points, and their launches; tree is null for the one.
+plora_status attend(const void* q, int64_t q_token, int64_t q_head, const plora_kv_cache* cache,
+                    const plora_kv_step* step, const plora_attn_shape* shape,
+                    const plora_tree* tree, float scale, const void* plan, size_t plan_bytes,
+                    void* out, int64_t out_token, int64_t out_head, void* ws, size_t ws_bytes,
+                    hipStream_t stream) {
   if (!cache || !step || !shape) return PLORA_ERR_INVALID_ARG;
+  if (tree && (tree->batch != step->batch || tree->T != step->T)) return PLORA_ERR_INVALID_ARG;
   const plora_attn_shape& s = *shape;
   const plora_kv_cache& c = *cache;
   if (s.batch < 0 || s.T < 0 || s.heads < 0 || s.kv_heads < 0 || s.max_q < 0 ||
@@ -962,10 +1048,12 @@ extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t
       c.head_stride % 8 || c.token_stride % 8 || c.token_stride >= kTokenStrideEnd)
     return PLORA_ERR_UNSUPPORTED;
   if (!q || !out || !plan || !ws || !step->pos || !step->req || !step->q_start ||
-      (c.n_pages > 0 && (!c.k || !c.v)) || (step->max_pages > 0 && !step->table))
+      (c.n_pages > 0 && (!c.k || !c.v)) || (step->max_pages > 0 && !step->table) ||
+      (tree && (!tree->span || !tree->info)))
     return PLORA_ERR_INVALID_ARG;
   if (!aligned(q, 16) || !aligned(out, 16) || !aligned(plan, 16) || !aligned(ws, 16) ||
-      !aligned(c.k, 16) || !aligned(c.v, 16))
+      !aligned(c.k, 16) || !aligned(c.v, 16) ||
+      (tree && (!aligned(tree->span, 8) || !aligned(tree->info, 8))))
     return PLORA_ERR_UNSUPPORTED;
   const Bounds b = bounds(s);
   const PlanLayout l = plan_layout(s, b);
@@ -1010,7 +1098,40 @@ extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t
   a.pm = reinterpret_cast<float*>(wp);
   a.pl = reinterpret_cast<float*>(wp + w.l);
   a.po = reinterpret_cast<float*>(wp + w.o);
-  if (c.dtype == PLORA_BF16)
-    return s.head_dim == 128 ? launch<Bf16, 128>(a, b, stream) : launch<Bf16, 64>(a, b, stream);
-  return s.head_dim == 128 ? launch<Fp16, 128>(a, b, stream) : launch<Fp16, 64>(a, b, stream);
+  if (tree) {
+    a.span = reinterpret_cast<const int2*>(tree->span);
+    a.tree = reinterpret_cast<const int2*>(tree->info);
+    return run<true>(a, b, s.head_dim, c.dtype, stream);
+  }
+  return run<false>(a, b, s.head_dim, c.dtype, stream);
+}
+
+}  // namespace
+}  // namespace paged
+
+extern "C" size_t plora_attn_paged_workspace_bytes(const plora_attn_shape* shape) {
+  using namespace paged;
+  if (!shape || !shape_ok(*shape) || shape_empty(*shape)) return 0;
+  return ws_layout(*shape, bounds(*shape)).bytes;
+}
+
+extern "C" plora_status plora_attn_paged(const void* q, int64_t q_token, int64_t q_head,
+                                         const plora_kv_cache* cache, const plora_kv_step* step,
+                                         const plora_attn_shape* shape, float scale,
+                                         const void* plan, size_t plan_bytes, void* out,
+                                         int64_t out_token, int64_t out_head, void* ws,
+                                         size_t ws_bytes, hipStream_t stream) {
+  return paged::attend(q, q_token, q_head, cache, step, shape, nullptr, scale, plan, plan_bytes,
+                       out, out_token, out_head, ws, ws_bytes, stream);
+}
+
+extern "C" plora_status plora_attn_tree(const void* q, int64_t q_token, int64_t q_head,
+                                        const plora_kv_cache* cache, const plora_kv_step* step,
+                                        const plora_attn_shape* shape, const plora_tree* tree,
+                                        float scale, const void* plan, size_t plan_bytes,
+                                        void* out, int64_t out_token, int64_t out_head, void* ws,
+                                        size_t ws_bytes, hipStream_t stream) {
+  if (!tree) return PLORA_ERR_INVALID_ARG;
+  return paged::attend(q, q_token, q_head, cache, step, shape, tree, scale, plan, plan_bytes,
+                       out, out_token, out_head, ws, ws_bytes, stream);
 }

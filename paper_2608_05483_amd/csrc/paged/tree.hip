@@ -1,0 +1,259 @@
+// Trees of drafted tokens (include/plora_tree.h): plora_tree_plan and
+// plora_tree_accept.  (plora_attn_tree is in attn_paged.hip.)
+
+#include <algorithm>
+
+#include "paged_dev.h"
+#include "plora_tree.h"
+
+namespace paged {
+namespace {
+
+constexpr int kNT = 256;
+constexpr int kWaves = kNT / 64;
+constexpr int kMost = PLORA_TREE_MAX_NODES;
+
+// The rows of request b, or (b = batch) those behind the last one; rows of no request
+// are those of a request that the step left out, too.
+struct Rows {
+  int q0, n;
+  bool there;
+};
+__device__ __forceinline__ Rows rows_of(const int32_t* q_start, const int32_t* req, int32_t batch,
+                                        int32_t T, int b) {
+  Rows x;
+  x.q0 = min(max(q_start[b], 0), T);
+  const int end = b < batch ? min(max(q_start[b + 1], 0), T) : T;
+  x.n = max(end - x.q0, 0);
+  x.there = b < batch && x.n > 0 && req[x.q0] == b;
+  return x;
+}
+
+struct TreeArgs {
+  const int32_t *parent, *q_start, *kv_len, *req;
+  int32_t batch, T;
+  int32_t* pos;
+  int2* span;
+  int2* info;
+};
+
+// A work group a request.  With the parents in LDS a node walks to its root three
+// times: for its depth, to add itself to the size of each of its ancestors, and to add
+// up the preorder number: one for each ancestor, and the sizes of the earlier siblings
+// of each node on the path, which are found by looking at the nodes between the parent
+// and the node.  Whole numbers, so the order of the additions changes nothing.
+// Bound by latency.
+__global__ __launch_bounds__(kNT) void tree_plan_kernel(TreeArgs a) {
+  __shared__ int s_par[kMost], s_size[kMost], s_sib[kMost];
+  __shared__ int s_chain[kWaves], s_cut;
+  const int tid = threadIdx.x, b = blockIdx.x;
+  const Rows x = rows_of(a.q_start, a.req, a.batch, a.T, b);
+  const int32_t* par = a.parent + x.q0;
+  if (tid == 0) s_cut = 0;
+  bool chain = true;
+  if (x.there)
+    for (int i = tid; i < x.n; i += kNT) {
+      const int p = par[i];
+      chain = chain && p == i - 1;
+      if (i < kMost) s_par[i] = p, s_size[i] = 0;
+    }
+  if ((tid & 63) == 0) s_chain[tid >> 6] = 1;
+  __syncthreads();
+  if (!chain) s_chain[tid >> 6] = 0;
+  __syncthreads();
+  for (int w = 0; w < kWaves; ++w) chain = chain && s_chain[w];
+  const int past = x.there ? max(a.kv_len[b] - x.n, 0) : 0;
+  if (!x.there || chain || x.n > kMost) {
+    const bool cut = !x.there || !chain;
+    for (int i = tid; i < x.n; i += kNT) {
+      a.pos[x.q0 + i] = cut ? 0 : past + i;
+      a.span[x.q0 + i] = cut ? int2{-1, -2} : int2{i, x.n - 1};
+    }
+    if (tid == 0 && b < a.batch)
+      a.info[b] = x.there && !chain ? int2{1, x.n} : int2{0, 0};
+    return;
+  }
+  int cut = 0;
+  for (int i = tid; i < x.n; i += kNT) {
+    int p = i, q = s_par[i];
+    while (q >= 0 && q < p) p = q, q = s_par[p];
+    if (q != -1) {
+      s_sib[i] = -1;
+      ++cut;
+      continue;
+    }
+    s_sib[i] = 0;
+    for (p = i; p >= 0; p = s_par[p]) atomicAdd(&s_size[p], 1);
+  }
+  if (cut) atomicAdd(&s_cut, cut);
+  __syncthreads();
+  for (int i = tid; i < x.n; i += kNT)
+    if (s_sib[i] == 0) {
+      const int p = s_par[i];
+      int before = 0;
+      for (int j = p + 1; j < i; ++j) before += s_par[j] == p ? s_size[j] : 0;
+      s_sib[i] = before;
+    }
+  __syncthreads();
+  for (int i = tid; i < x.n; i += kNT) {
+    int pos = 0;
+    int2 span = {-1, -2};
+    if (s_sib[i] >= 0) {
+      int depth = -1, first = 0;
+      for (int p = i; p >= 0; p = s_par[p]) ++depth, first += s_sib[p];
+      first += depth;
+      pos = past + depth;
+      span = int2{first, first + s_size[i] - 1};
+    }
+    a.pos[x.q0 + i] = pos;
+    a.span[x.q0 + i] = span;
+  }
+  if (tid == 0) a.info[b] = int2{1, s_cut};
+}
+
+struct AcceptArgs {
+  const int32_t* parent;
+  const void *drafted, *target;
+  const int32_t *given, *q_start, *kv_len, *req;
+  int32_t batch, T;
+  int32_t *path, *count;
+  void* token;
+  int32_t* kv_out;
+};
+
+// A wavefront a request.  A child has a higher number than its node, so the search for
+// the next node begins behind the present one, 64 nodes at a time, and the first lane
+// that fits has the lowest number.  Bound by latency.
+template <class Tok>
+__global__ __launch_bounds__(kNT) void tree_accept_kernel(AcceptArgs a) {
+  const int lane = threadIdx.x & 63, b = blockIdx.x * kWaves + (threadIdx.x >> 6);
+  if (b > a.batch) return;
+  const Rows x = rows_of(a.q_start, a.req, a.batch, a.T, b);
+  const int32_t* par = a.parent + x.q0;
+  const Tok* drafted = static_cast<const Tok*>(a.drafted) + x.q0;
+  const Tok* target = static_cast<const Tok*>(a.target) + x.q0;
+  int32_t* path = a.path + x.q0;
+  int count = 0;
+  Tok token = -1;
+  if (x.there) {
+    count = a.given ? min(max(a.given[b], 0), x.n) : 1;
+    for (int i = lane; i < count; i += 64) path[i] = i;
+    // nodes are cut if there are too many, and no path goes on from a cut node: one of
+    // the given ones, whose ancestors are all among them
+    bool going = count > 0;
+    if (going && x.n > kMost) {
+      bool chain = true;
+      for (int i = lane; i < x.n; i += 64) chain = chain && par[i] == i - 1;
+      going = __all(chain);
+    }
+    if (going) {
+      bool fine = true;
+      for (int i = lane; i < count; i += 64) fine = fine && par[i] >= -1 && par[i] < i;
+      if (!__all(fine)) {
+        int p = count - 1, q = par[p];
+        while (q >= 0 && q < p) p = q, q = par[p];
+        going = q == -1;
+      }
+    }
+    int cur = count - 1;
+    while (going) {
+      const Tok want = target[cur];
+      going = false;
+      for (int i0 = cur + 1; i0 < x.n; i0 += 64) {
+        const int i = i0 + lane;
+        const uint64_t fits = __ballot(i < x.n && par[i] == cur && drafted[i] == want);
+        if (fits) {
+          cur = i0 + __builtin_ctzll(fits);
+          if (lane == 0) path[count] = cur;
+          ++count;
+          going = true;
+          break;
+        }
+      }
+    }
+    if (count > 0) token = target[cur];
+  }
+  for (int i = count + lane; i < x.n; i += 64) path[i] = -1;
+  if (lane == 0 && b < a.batch) {
+    a.count[b] = count;
+    static_cast<Tok*>(a.token)[b] = token;
+    a.kv_out[b] = a.kv_len[b] - (x.there ? x.n - count : 0);
+  }
+}
+
+plora_status step_status(const plora_kv_step* s) {
+  if (!s || s->batch < 0 || s->T < 0) return PLORA_ERR_INVALID_ARG;
+  if (s->batch > PLORA_PAGED_MAX_BATCH || s->T > PLORA_PAGED_MAX_TOKENS)
+    return PLORA_ERR_UNSUPPORTED;
+  if (s->batch == 0 && s->T == 0) return PLORA_OK;
+  if (!s->q_start || (s->batch > 0 && !s->kv_len) || (s->T > 0 && !s->req))
+    return PLORA_ERR_INVALID_ARG;
+  return PLORA_OK;
+}
+
+}  // namespace
+}  // namespace paged
+
+extern "C" plora_status plora_tree_plan(const int32_t* parent, const plora_kv_step* step,
+                                        const plora_tree* tree, hipStream_t stream) {
+  using namespace paged;
+  const plora_status st = step_status(step);
+  if (st != PLORA_OK) return st;
+  if (!tree || tree->batch != step->batch || tree->T != step->T) return PLORA_ERR_INVALID_ARG;
+  if (step->batch == 0 && step->T == 0) return PLORA_OK;
+  if ((step->T > 0 && (!parent || !tree->pos || !tree->span)) || (step->batch > 0 && !tree->info))
+    return PLORA_ERR_INVALID_ARG;
+  if (!aligned(tree->span, 8) || !aligned(tree->info, 8)) return PLORA_ERR_UNSUPPORTED;
+  TreeArgs a{};
+  a.parent = parent;
+  a.q_start = step->q_start;
+  a.kv_len = step->kv_len;
+  a.req = step->req;
+  a.batch = step->batch;
+  a.T = step->T;
+  a.pos = tree->pos;
+  a.span = reinterpret_cast<int2*>(tree->span);
+  a.info = reinterpret_cast<int2*>(tree->info);
+  clear_error();
+  hipLaunchKernelGGL(tree_plan_kernel, dim3(step->batch + 1), dim3(kNT), 0, stream, a);
+  return launch_status();
+}
+
+extern "C" plora_status plora_tree_accept(const int32_t* parent, const void* drafted,
+                                          const void* target, int32_t token_bytes,
+                                          const int32_t* given, const plora_kv_step* step,
+                                          int32_t* path, int32_t* count, void* token,
+                                          int32_t* kv_len, hipStream_t stream) {
+  using namespace paged;
+  const plora_status st = step_status(step);
+  if (st != PLORA_OK) return st;
+  if (token_bytes != 4 && token_bytes != 8) return PLORA_ERR_UNSUPPORTED;
+  if (step->batch == 0 && step->T == 0) return PLORA_OK;
+  if ((step->T > 0 && (!parent || !drafted || !target || !path)) ||
+      (step->batch > 0 && (!count || !token || !kv_len)))
+    return PLORA_ERR_INVALID_ARG;
+  if (!aligned(drafted, token_bytes) || !aligned(target, token_bytes) ||
+      !aligned(token, token_bytes))
+    return PLORA_ERR_UNSUPPORTED;
+  AcceptArgs a{};
+  a.parent = parent;
+  a.drafted = drafted;
+  a.target = target;
+  a.given = given;
+  a.q_start = step->q_start;
+  a.kv_len = step->kv_len;
+  a.req = step->req;
+  a.batch = step->batch;
+  a.T = step->T;
+  a.path = path;
+  a.count = count;
+  a.token = token;
+  a.kv_out = kv_len;
+  const dim3 grid((step->batch + kWaves) / kWaves);        // and the rows behind the last
+  clear_error();
+  if (token_bytes == 4)
+    hipLaunchKernelGGL(tree_accept_kernel<int32_t>, grid, dim3(kNT), 0, stream, a);
+  else
+    hipLaunchKernelGGL(tree_accept_kernel<int64_t>, grid, dim3(kNT), 0, stream, a);
+  return launch_status();
+}
