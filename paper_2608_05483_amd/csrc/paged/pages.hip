@@ -1,0 +1,484 @@
+// Upkeep of a paged cache (include/plora_pages.h): plora_kv_remap, plora_kv_copy,
+// plora_kv_compact.
+
+#include <algorithm>
+
+#include "paged_dev.h"
+#include "plora_pages.h"
+
+namespace paged {
+namespace {
+
+constexpr int kNT = 256;
+
+struct RemapArgs {
+  const int32_t *old_table, *old_len, *src, *keep, *free_head;
+  int32_t *new_table, *new_len, *shares, *free_pages, *free_next, *copies, *meta;
+  int32_t old_batch, new_batch, old_max, new_max, log_page, n_pages, n_free;
+  // workspace: a new request's partly filled page (-1: none), and the entries that an
+  // old one drops; scratch: for such pages who holds them so (how many, the last)
+  int32_t* part;
+  int2 *drop, *last;
+};
+
+__device__ __forceinline__ int old_length(const RemapArgs& a, int b) {
+  return (int)min((int64_t)max(a.old_len[b], 0), (int64_t)a.old_max << a.log_page);
+}
+// Keys that new request i holds.
+__device__ __forceinline__ int new_length(const RemapArgs& a, int i, int b) {
+  if (b < 0 || b >= a.old_batch) return 0;
+  int n = old_length(a, b);
+  if (a.keep) n = min(n, max(a.keep[i], 0));
+  return (int)min((int64_t)n, (int64_t)a.new_max << a.log_page);
+}
+__device__ __forceinline__ int pages_of(const RemapArgs& a, int keys) {
+  return (keys + (1 << a.log_page) - 1) >> a.log_page;
+}
+__device__ __forceinline__ bool in_pool(const RemapArgs& a, int page) {
+  return page >= 0 && page < a.n_pages;
+}
+__device__ __forceinline__ int now(const int32_t* p) {
+  return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// The lowest of the work group's values.
+__device__ __forceinline__ int lowest(int x, int* red) {
+#pragma unroll
+  for (int d = 32; d; d >>= 1) x = min(x, __shfl_xor(x, d, 64));
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kNT / 64; ++w) x = min(x, red[w]);
+  return x;
+}
+
+// A work group for each new and each old request.  An old request's holds pass to the
+// first new one that continues it, so only what changes is counted: that one's shorter
+// tail and the pages of requests that none continues are dropped, the other
+// continuations hold theirs in addition.  Sums of whole numbers, in any order.
+__global__ __launch_bounds__(kNT) void remap_rows_kernel(RemapArgs a) {
+  __shared__ int red[kNT / 64];
+  const int tid = threadIdx.x, i = blockIdx.x;
+  if (i < a.new_batch) {
+    const int b = a.src[i], n = new_length(a, i, b), pages = pages_of(a, n);
+    if (tid == 0) {
+      a.new_len[i] = n;
+      if (pages == 0) a.part[i] = -1;
+    }
+    if (pages == 0) return;
+    int first = i;
+    for (int j = tid; j < i; j += kNT)
+      if (a.src[j] == b) first = min(first, j);
+    first = lowest(first, red);
+    const int32_t* from = a.old_table + (int64_t)b * a.old_max;
+    int32_t* to = a.new_table + (int64_t)i * a.new_max;
+    for (int j = tid; j < pages; j += kNT) {
+      const int page = from[j];
+      const bool held = in_pool(a, page);
+      to[j] = page;
+      if (first < i && held) atomicAdd(&a.shares[page], 1);
+      if (j == pages - 1) {
+        const bool part = held && (n & ((1 << a.log_page) - 1));
+        a.part[i] = part ? page : -1;
+        if (part) a.last[page] = int2{0, -1};
+      }
+    }
+  } else {
+    const int b = i - a.new_batch;
+    int first = a.new_batch;
+    for (int j = tid; j < a.new_batch; j += kNT)
+      if (a.src[j] == b) first = min(first, j);
+    first = lowest(first, red);
+    const int kept = first < a.new_batch ? pages_of(a, new_length(a, first, b)) : 0;
+    const int held = pages_of(a, old_length(a, b));
+    if (tid == 0) a.drop[b] = int2{kept, held - kept};
+    const int32_t* from = a.old_table + (int64_t)b * a.old_max;
+    for (int j = kept + tid; j < held; j += kNT) {
+      const int page = from[j];
+      if (in_pool(a, page)) atomicAdd(&a.shares[page], -1);
+    }
+  }
+}
+
+constexpr int kFT = 1024;                // threads, and requests looked at together
+constexpr int kFW = kFT / 64;
+
+// Exclusive sum over the work group's threads; total is the sum of all.
+__device__ __forceinline__ int block_sum(int x, int* red, int& total) {
+  const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
+  const int inc = wave_scan(x, Add{});
+  __syncthreads();
+  if (lane == 63) red[wv] = inc;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kFW; ++w) {
+    if (w < wv) before += red[w];
+    total += red[w];
+  }
+  return before + inc - x;
+}
+
+// One work group.  The entries that old requests drop, 1024 requests and 1024 entries
+// at a time: of those whose page nobody holds (its count is below 0) the lowest request
+// puts its mark there, and the marked ones go before the list's head, from the last to
+// the first.  Then the new requests' partly filled pages: how many hold a page so and
+// which is the last of them are known after one pass, so each can tell whether it has
+// to take a page of its own; a scan numbers those that do.
+// Bound by latency: dependent loads and barriers.
+__global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
+  __shared__ int s_first[kFT], s_from[kFT];
+  __shared__ int red[kFW];
+  constexpr int kMark = INT32_MIN / 2;   // (a request's number is added)
+  const int tid = threadIdx.x;
+  const int head = *a.free_head;
+  const bool list = head >= 0 && head <= a.n_free;
+  int room = list ? head : 0, freed = 0;
+  const int chunks = (a.old_batch + kFT - 1) / kFT;
+  // visits entry after entry: f(request, page or -1, its turn)
+  const auto chunk = [&](int c, auto&& f, bool back) {
+    const int b0 = c * kFT, m = min(kFT, a.old_batch - b0);
+    const int2 d = tid < m ? a.drop[b0 + tid] : int2{0, 0};
+    int total;
+    s_first[tid] = block_sum(d.y, red, total);
+    s_from[tid] = d.x;
+    __syncthreads();
+    const int turns = (total + kFT - 1) / kFT;
+    for (int t = 0; t < turns; ++t) {
+      const int e = (back ? turns - 1 - t : t) * kFT + tid;
+      int b = -1, page = -1;
+      if (e < total) {
+        int lo = 0, hi = m;              // the last request that starts at or before e
+        while (hi - lo > 1) {
+          const int mid = (lo + hi) >> 1;
+          if (s_first[mid] <= e) lo = mid;
+          else hi = mid;
+        }
+        b = b0 + lo;
+        page = a.old_table[(int64_t)b * a.old_max + s_from[lo] + e - s_first[lo]];
+        if (!in_pool(a, page)) page = -1;
+      }
+      f(b, page);
+    }
+    __syncthreads();
+  };
+  for (int c = 0; c < chunks; ++c)
+    chunk(c, [&](int b, int page) {
+      if (page >= 0 && now(&a.shares[page]) < 0) atomicMin(&a.shares[page], kMark + b);
+    }, false);
+  for (int c = chunks - 1; c >= 0; --c)
+    chunk(c, [&](int b, int page) {
+      const bool mine = page >= 0 && now(&a.shares[page]) == kMark + b;
+      int total;
+      const int before = block_sum(mine, red, total);
+      // (the last of this turn is put right before the head)
+      const int at = room - total + before;
+      if (mine) {
+        a.shares[page] = 0;
+        if (at >= 0) a.free_pages[at] = page;
+      }
+      room -= total;
+      freed += total;
+    }, true);
+  const int put = min(freed, list ? head : 0), top = head - put;
+  const int avail = list ? a.n_free - top : 0;
+  __threadfence();
+  __syncthreads();
+  // partly filled pages
+  for (int i = tid; i < a.new_batch; i += kFT) {
+    const int page = a.part[i];
+    if (page >= 0) atomicAdd(&a.last[page].x, 1), atomicMax(&a.last[page].y, i);
+  }
+  __syncthreads();
+  int taken = 0;
+  for (int i0 = 0; i0 < a.new_batch; i0 += kFT) {
+    const int i = i0 + tid;
+    const int page = i < a.new_batch ? a.part[i] : -1;
+    bool own = false;
+    if (page >= 0) {
+      const int holders = now(&a.shares[page]) + 1;
+      own = holders > 1 && (now(&a.last[page].x) != holders || now(&a.last[page].y) != i);
+    }
+    int total;
+    const int at = taken + block_sum(own, red, total);
+    taken += total;
+    if (own) {
+      const int n = a.new_len[i], S1 = (1 << a.log_page) - 1;
+      if (at < avail) {
+        const int fresh = now(&a.free_pages[top + at]);
+        a.new_table[(int64_t)i * a.new_max + (n >> a.log_page)] = fresh;
+        a.copies[3 * at] = page;
+        a.copies[3 * at + 1] = fresh;
+        a.copies[3 * at + 2] = n & S1;
+      } else {
+        a.new_len[i] = n & ~S1;
+      }
+    }
+  }
+  // (counts change once nobody asks for them any more)
+  __syncthreads();
+  const int given = min(taken, max(avail, 0));
+  for (int i = tid; i < a.new_batch; i += kFT) {
+    const int page = a.part[i];
+    if (page >= 0) {
+      const int2 l = {now(&a.last[page].x), now(&a.last[page].y)};
+      // all that held it so took pages of their own, but the last if nobody else holds it
+      if (l.y == i) {
+        const int holders = now(&a.shares[page]) + 1;
+        if (holders > 1) a.shares[page] = holders - 1 - (l.x == holders ? l.x - 1 : l.x);
+      }
+    }
+    if (i >= given) a.copies[3 * i] = a.copies[3 * i + 1] = a.copies[3 * i + 2] = -1;
+  }
+  if (tid == 0) {
+    *a.free_next = top + given;
+    a.meta[0] = put;
+    a.meta[1] = given;
+    a.meta[2] = taken - given;
+    a.meta[3] = freed - put;
+  }
+  if (tid >= 4 && tid < 8) a.meta[tid] = 0;
+}
+
+// Layers of one launch; their pointers are the launch's arguments.
+constexpr int kLayers = 64;
+struct MoveArgs {
+  uint8_t* pool[2 * kLayers];            // k and v by layer
+  int64_t page_stride, head_stride, token_stride;   // bytes
+  int32_t n_pages, log_page, kv_heads, units;       // units of a row
+};
+
+template <class U>
+__device__ __forceinline__ U* at(const MoveArgs& a, uint8_t* pool, int64_t page, int key) {
+  return reinterpret_cast<U*>(pool + page * a.page_stride + key * a.token_stride);
+}
+
+// A work group copies a page's keys in k or v of a layer: neighbouring threads take
+// neighbouring units of a row, then the rows of a head, then the heads.  Bound by
+// reading and writing.
+template <class U>
+__global__ __launch_bounds__(kNT) void copy_kernel(MoveArgs a, const int32_t* copies, int32_t cap,
+                                                   const int32_t* n_copies) {
+  const int e = blockIdx.x;
+  if (e >= min(*n_copies, cap)) return;
+  const int from = copies[3 * e], to = copies[3 * e + 1];
+  const int keys = min(copies[3 * e + 2], 1 << a.log_page);
+  if (from < 0 || from >= a.n_pages || to < 0 || to >= a.n_pages || keys <= 0) return;
+  uint8_t* pool = a.pool[2 * blockIdx.y + blockIdx.z];
+  const U* x = at<U>(a, pool, from, 0);
+  U* y = at<U>(a, pool, to, 0);
+  const int per_head = keys * a.units, n = per_head * a.kv_heads;
+  for (int i = threadIdx.x; i < n; i += kNT) {
+    const int h = i / per_head, j = i - h * per_head, key = j / a.units, u = j - key * a.units;
+    const int64_t off = h * a.head_stride + key * a.token_stride + (int64_t)u * sizeof(U);
+    *reinterpret_cast<U*>(reinterpret_cast<uint8_t*>(y) + off) =
+        *reinterpret_cast<const U*>(reinterpret_cast<const uint8_t*>(x) + off);
+  }
+}
+
+// A thread moves one unit of a head's row, in k or v of a layer, for all keys of a
+// request's path one after the other; what it moves nobody else touches, and a path's
+// numbers rise, so no key is overwritten before it is read.  Bound by latency.
+template <class U>
+__global__ __launch_bounds__(kNT) void compact_kernel(MoveArgs a, const int32_t* q_start,
+                                                      const int32_t* req, const int64_t* slot,
+                                                      const int32_t* path, const int32_t* count,
+                                                      int32_t T, int32_t parts) {
+  const int b = blockIdx.x / parts, c = (blockIdx.x % parts) * kNT + threadIdx.x;
+  const int q0 = max(q_start[b], 0), n = min(q_start[b + 1], T) - q0;
+  if (n <= 0 || req[q0] != b || c >= a.kv_heads * a.units) return;
+  const int m = min(count[b], n), S1 = (1 << a.log_page) - 1;
+  const int64_t slots = (int64_t)a.n_pages << a.log_page;
+  uint8_t* pool = a.pool[2 * blockIdx.y + blockIdx.z] + (c / a.units) * a.head_stride +
+                  (int64_t)(c % a.units) * sizeof(U);
+  for (int i = 0; i < m; ++i) {
+    const int j = path[q0 + i];
+    if (j == i || j < 0 || j >= n) continue;
+    const int64_t from = slot[q0 + j], to = slot[q0 + i];
+    if (from < 0 || from >= slots || to < 0 || to >= slots) continue;
+    *at<U>(a, pool, to >> a.log_page, (int)to & S1) =
+        *at<U>(a, pool, from >> a.log_page, (int)from & S1);
+  }
+}
+
+// The layers' checks, and what a launch needs of them; *bytes is the widest unit that
+// all rows are made of.
+plora_status caches_status(const plora_kv_cache* c, int32_t layers, MoveArgs& a, int& bytes) {
+  if (layers < 0 || (layers > 0 && !c)) return PLORA_ERR_INVALID_ARG;
+  if (layers > PLORA_CACHE_MAX_LAYERS) return PLORA_ERR_UNSUPPORTED;
+  if (layers == 0) return PLORA_OK;
+  const plora_kv_cache& x = c[0];
+  if (x.n_pages < 0 || x.kv_heads < 0 || x.head_dim < 0 || x.page_stride < 0 ||
+      x.head_stride < 0 || x.token_stride < 0)
+    return PLORA_ERR_INVALID_ARG;
+  if (!page_size_ok(x.page_size) || (x.dtype != PLORA_BF16 && x.dtype != PLORA_FP16) ||
+      x.kv_heads > 1024 || x.head_dim > PLORA_ROPE_MAX_DIM)
+    return PLORA_ERR_UNSUPPORTED;
+  uint64_t bits = (uint64_t)x.page_stride | (uint64_t)x.head_stride | (uint64_t)x.token_stride |
+                  (uint64_t)x.head_dim;
+  bits *= 2;
+  for (int l = 0; l < layers; ++l) {
+    const plora_kv_cache& y = c[l];
+    if (y.n_pages != x.n_pages || y.page_size != x.page_size || y.kv_heads != x.kv_heads ||
+        y.head_dim != x.head_dim || y.dtype != x.dtype || y.page_stride != x.page_stride ||
+        y.head_stride != x.head_stride || y.token_stride != x.token_stride)
+      return PLORA_ERR_INVALID_ARG;
+    if (x.n_pages > 0 && x.kv_heads > 0 && x.head_dim > 0 && (!y.k || !y.v))
+      return PLORA_ERR_INVALID_ARG;
+    bits |= reinterpret_cast<uintptr_t>(y.k) | reinterpret_cast<uintptr_t>(y.v);
+  }
+  bytes = bits & 1 ? 1 : bits & 2 ? 2 : bits & 4 ? 4 : bits & 8 ? 8 : 16;
+  if (bytes == 1) return PLORA_ERR_UNSUPPORTED;
+  a.page_stride = x.page_stride * 2;
+  a.head_stride = x.head_stride * 2;
+  a.token_stride = x.token_stride * 2;
+  a.n_pages = x.n_pages;
+  a.log_page = log2_of(x.page_size);
+  a.kv_heads = x.kv_heads;
+  a.units = x.head_dim * 2 / bytes;
+  return PLORA_OK;
+}
+
+// f<U>(layers of this launch) for all layers, kLayers at a time.
+template <class F>
+plora_status by_layers(const plora_kv_cache* c, int32_t layers, MoveArgs& a, int bytes, F&& f) {
+  clear_error();
+  for (int l0 = 0; l0 < layers; l0 += kLayers) {
+    const int n = std::min(kLayers, layers - l0);
+    for (int l = 0; l < n; ++l) {
+      a.pool[2 * l] = static_cast<uint8_t*>(c[l0 + l].k);
+      a.pool[2 * l + 1] = static_cast<uint8_t*>(c[l0 + l].v);
+    }
+    if (bytes == 16) f(u32x4{}, n);
+    else if (bytes == 8) f(u32x2{}, n);
+    else if (bytes == 4) f(uint32_t{}, n);
+    else f(uint16_t{}, n);
+    const plora_status st = launch_status();
+    if (st != PLORA_OK) return st;
+  }
+  return PLORA_OK;
+}
+
+struct RemapWs {
+  size_t drop, bytes;
+};
+RemapWs remap_ws(int32_t old_batch, int32_t new_batch) {
+  RemapWs w{};
+  w.drop = align256((size_t)new_batch * 4);
+  w.bytes = w.drop + align256((size_t)old_batch * 8);
+  return w;
+}
+
+}  // namespace
+}  // namespace paged
+
+extern "C" size_t plora_kv_remap_workspace_bytes(int32_t old_batch, int32_t new_batch) {
+  if (old_batch < 0 || new_batch < 0 || old_batch > PLORA_PAGED_MAX_BATCH ||
+      new_batch > PLORA_PAGED_MAX_BATCH)
+    return 0;
+  return paged::remap_ws(old_batch, new_batch).bytes;
+}
+
+extern "C" plora_status plora_kv_remap(const plora_kv_batch* old_batch, const int32_t* src,
+                                       const int32_t* keep, int32_t page_size,
+                                       const plora_page_pool* pool, const int32_t* free_head,
+                                       int32_t* free_next, const plora_kv_batch* new_batch,
+                                       int32_t* copies, int32_t* meta, void* ws, size_t ws_bytes,
+                                       hipStream_t stream) {
+  using namespace paged;
+  if (!old_batch || !new_batch || !pool) return PLORA_ERR_INVALID_ARG;
+  const plora_kv_batch &o = *old_batch, &n = *new_batch;
+  if (o.batch < 0 || o.max_pages < 0 || n.batch < 0 || n.max_pages < 0 || pool->n_pages < 0 ||
+      pool->n_free < 0)
+    return PLORA_ERR_INVALID_ARG;
+  if (o.batch > PLORA_PAGED_MAX_BATCH || n.batch > PLORA_PAGED_MAX_BATCH ||
+      !page_size_ok(page_size) || (int64_t)o.max_pages * page_size > PLORA_PAGED_MAX_KEYS ||
+      (int64_t)n.max_pages * page_size > PLORA_PAGED_MAX_KEYS)
+    return PLORA_ERR_UNSUPPORTED;
+  if (!free_head || !free_next || !meta || (o.batch + n.batch > 0 && !ws) || (pool->n_pages > 0 && (!pool->shares || !pool->scratch)) ||
+      (pool->n_free > 0 && !pool->free_pages) || (o.batch > 0 && !o.kv_len) ||
+      (o.batch > 0 && o.max_pages > 0 && !o.table) ||
+      (n.batch > 0 && (!n.kv_len || !src || !copies)) ||
+      (n.batch > 0 && n.max_pages > 0 && !n.table))
+    return PLORA_ERR_INVALID_ARG;
+  if (!aligned(ws, 16) || !aligned(pool->scratch, 8)) return PLORA_ERR_UNSUPPORTED;
+  const RemapWs w = remap_ws(o.batch, n.batch);
+  if (ws_bytes < w.bytes) return PLORA_ERR_WORKSPACE_TOO_SMALL;
+  RemapArgs a{};
+  a.old_table = o.table;
+  a.old_len = o.kv_len;
+  a.src = src;
+  a.keep = keep;
+  a.free_head = free_head;
+  a.new_table = n.table;
+  a.new_len = n.kv_len;
+  a.shares = pool->shares;
+  a.free_pages = pool->free_pages;
+  a.free_next = free_next;
+  a.copies = copies;
+  a.meta = meta;
+  a.old_batch = o.batch;
+  a.new_batch = n.batch;
+  a.old_max = o.max_pages;
+  a.new_max = n.max_pages;
+  a.log_page = log2_of(page_size);
+  a.n_pages = pool->n_pages;
+  a.n_free = pool->n_free;
+  char* p = static_cast<char*>(ws);
+  a.part = reinterpret_cast<int32_t*>(p);
+  a.drop = reinterpret_cast<int2*>(p + w.drop);
+  a.last = reinterpret_cast<int2*>(pool->scratch);
+  clear_error();
+  if (o.batch + n.batch > 0) {
+    hipLaunchKernelGGL(remap_rows_kernel, dim3(o.batch + n.batch), dim3(kNT), 0, stream, a);
+    const plora_status st = launch_status();
+    if (st != PLORA_OK) return st;
+  }
+  hipLaunchKernelGGL(remap_finish_kernel, dim3(1), dim3(kFT), 0, stream, a);
+  return launch_status();
+}
+
+extern "C" plora_status plora_kv_copy(const plora_kv_cache* caches, int32_t layers,
+                                      const int32_t* copies, int32_t cap,
+                                      const int32_t* n_copies, hipStream_t stream) {
+  using namespace paged;
+  if (cap < 0) return PLORA_ERR_INVALID_ARG;
+  if (cap > PLORA_PAGED_MAX_BATCH) return PLORA_ERR_UNSUPPORTED;
+  MoveArgs a{};
+  int bytes = 16;
+  const plora_status st = caches_status(caches, layers, a, bytes);
+  if (st != PLORA_OK) return st;
+  if (cap > 0 && (!copies || !n_copies)) return PLORA_ERR_INVALID_ARG;
+  if (cap == 0 || layers == 0 || a.n_pages == 0 || a.kv_heads == 0 || a.units == 0)
+    return PLORA_OK;
+  return by_layers(caches, layers, a, bytes, [&](auto u, int n) {
+    hipLaunchKernelGGL(copy_kernel<decltype(u)>, dim3(cap, n, 2), dim3(kNT), 0, stream, a, copies,
+                       cap, n_copies);
+  });
+}
+
+extern "C" plora_status plora_kv_compact(const plora_kv_cache* caches, int32_t layers,
+                                         const plora_kv_step* step, const int32_t* path,
+                                         const int32_t* count, hipStream_t stream) {
+  using namespace paged;
+  if (!step || step->batch < 0 || step->T < 0) return PLORA_ERR_INVALID_ARG;
+  if (step->batch > PLORA_PAGED_MAX_BATCH || step->T > PLORA_PAGED_MAX_TOKENS)
+    return PLORA_ERR_UNSUPPORTED;
+  MoveArgs a{};
+  int bytes = 16;
+  const plora_status st = caches_status(caches, layers, a, bytes);
+  if (st != PLORA_OK) return st;
+  if (layers > 0 && caches[0].page_size != step->page_size) return PLORA_ERR_INVALID_ARG;
+  if (step->batch == 0 || step->T == 0 || layers == 0 || a.n_pages == 0 || a.kv_heads == 0 ||
+      a.units == 0)
+    return PLORA_OK;
+  if (!step->q_start || !step->req || !step->slot || !path || !count)
+    return PLORA_ERR_INVALID_ARG;
+  const int parts = (a.kv_heads * a.units + kNT - 1) / kNT;
+  return by_layers(caches, layers, a, bytes, [&](auto u, int n) {
+    hipLaunchKernelGGL(compact_kernel<decltype(u)>, dim3(step->batch * parts, n, 2), dim3(kNT), 0,
+                       stream, a, step->q_start, step->req, step->slot, path, count, step->T,
+                       parts);
+  });
+}
