@@ -144,7 +144,7 @@ __device__ __forceinline__ NewKeys new_keys(const AttnArgs& a, const Item& it) {
   NewKeys x{INT32_MAX, 0};
   if constexpr (TREE) {
     if (!it.gathered && a.tree[it.req].x) {
-      x.past = a.pos[it.tok];
+      x.past = uniform(a.pos[it.tok]);
       x.shift = x.past - it.tok;
     }
   }
@@ -155,9 +155,9 @@ __device__ __forceinline__ NewKeys new_keys(const AttnArgs& a, const Item& it) {
 template <bool TREE>
 __device__ __forceinline__ bool sees(const AttnArgs& a, const NewKeys& fresh, const Row& x,
                                      int key) {
-  if (!TREE || key < fresh.past) return true;
+  if (!TREE) return true;
   const int2 s = a.span[min(max(key - fresh.shift, 0), a.T - 1)];
-  return s.x <= x.number && x.number <= s.y;
+  return (key < fresh.past) | ((s.x <= x.number) & (x.number <= s.y));
 }
 
 // One row by itself, in vector arithmetic over the keys it sees and no others,
@@ -353,9 +353,13 @@ __device__ __forceinline__ void few_item(const AttnArgs& a, const Item& it, int 
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int key = k0 + 16 * (i >> 2) + 4 * g + (i & 3);
-        const bool seen = key < x.limit && sees<TREE>(a, fresh, x, key);
+        bool seen = key < x.limit;
+        if constexpr (TREE) {
+          const bool in = sees<TREE>(a, fresh, x, key);
+          seen = seen & in;
+          some = some | seen;
+        }
         t[i] = seen ? t[i] : -INFINITY;
-        if constexpr (TREE) some = some || seen;
       }
     }
     float mx = m;
@@ -534,7 +538,7 @@ __device__ __forceinline__ void loads_done() { __builtin_amdgcn_s_waitcnt(0x0f70
 template <class Ty, int D, bool TWO, bool TREE>
 __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int kvh,
                                           int* s_most, u32x4* s_k0, u32x4* s_k1, u32x4* s_v0,
-                                          u32x4* s_v1) {
+                                          u32x4* s_v1, int* s_n0, int* s_n1) {
   constexpr int kQ = D / 16;                // products over a row
   constexpr int kV = D / 32;                // tiles of the output's dimensions
   constexpr int kU = D / 8;                 // 16-byte units of a row
@@ -600,8 +604,19 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
   const int kg = uniform(kr >> 4), ko = kr & 15;
   const int off_k = (ko * a.key_stride + 8 * (ku ^ (kr & (kU - 1)))) * 2;
   const int off_v = (ko * a.key_stride + 8 * (ku ^ turn_v(kr))) * 2;
-  const auto fetch = [&](int t, u32x4* sk, u32x4* sv) {
+  const auto fetch = [&](int t, u32x4* sk, u32x4* sv, int* sn) {
     if ((t & 15) == 0) locate(it.lo + t * kTileStep);
+    if constexpr (TREE) {
+      // the intervals of 64 keys, firsts and lasts (what is none of the step's tokens
+      // reads zero, and is cached or behind the end)
+      if (wv == 0 && it.lo + (t + 1) * kTileStep > fresh.past) {
+        const auto r = __builtin_amdgcn_make_buffer_rsrc(const_cast<int2*>(a.span), 0, a.T * 8,
+                                                         kRsrcWord3);
+        const int off = (it.lo + t * kTileStep + lane - fresh.shift) * 8;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)sn, 4, off, 0, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_ptr)(sn + 64), 4, off + 4, 0, 0, 0);
+      }
+    }
     const int j0 = 4 * (t & 15);
 #pragma unroll
     for (int i = 0; i < kKL; ++i) {
@@ -625,13 +640,14 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
     for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
   if (tiles > 0) {
     ask(it.lo);
-    fetch(0, s_k0, s_v0);
+    fetch(0, s_k0, s_v0, s_n0);
     loads_done();
   }
   __syncthreads();
-  const auto step = [&](int t, const u32x4* sk, const u32x4* sv, u32x4* nk, u32x4* nv) {
+  const auto step = [&](int t, const u32x4* sk, const u32x4* sv, const int* sn, u32x4* nk,
+                        u32x4* nv, int* nn) {
     const int k0 = it.lo + t * kTileStep;
-    if (t + 1 < tiles) fetch(t + 1, nk, nv);
+    if (t + 1 < tiles) fetch(t + 1, nk, nv, nn);
     if (t < my) {
       const u32x4* kp = sk + n * kU;
       const int kx = h ^ (n & (kU - 1));
@@ -654,29 +670,28 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
       __builtin_amdgcn_sched_barrier(0);
       if (k0 + kTileStep > least) {
         const int lim = x.limit - k0 - 4 * h;
+        if (!TREE || k0 + kTileStep <= fresh.past) {
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+          for (int b = 0; b < 2; ++b)
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            s[b][i] = 32 * b + 8 * (i >> 2) + (i & 3) < lim ? s[b][i] : -INFINITY;
-        if constexpr (TREE) {
-          if (k0 + kTileStep > fresh.past) {
-            // bit 16 b + i: whether s[b][i] is seen, four keys in a row at a time
-            uint32_t seen = 0;
-#pragma unroll 1
-            for (int j = 0; j < 8; ++j)
+            for (int i = 0; i < 16; ++i)
+              s[b][i] = 32 * b + 8 * (i >> 2) + (i & 3) < lim ? s[b][i] : -INFINITY;
+          if constexpr (TREE) any = any || lim > 0;
+        } else {
+          const int cached = fresh.past - k0 - 4 * h;
+          const i32x4* np = reinterpret_cast<const i32x4*>(sn) + h;
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
-                seen |= (uint32_t)(8 * j + e < lim && sees<TREE>(a, fresh, x, k0 + 4 * h + 8 * j + e))
-                        << (4 * j + e);
-            any = any || seen;
+          for (int j = 0; j < 8; ++j) {
+            const i32x4 first = np[2 * j], last = np[16 + 2 * j];
 #pragma unroll
-            for (int b = 0; b < 2; ++b)
-#pragma unroll
-              for (int i = 0; i < 16; ++i)
-                s[b][i] = seen >> (16 * b + i) & 1 ? s[b][i] : -INFINITY;
-          } else {
-            any = any || lim > 0;
+            for (int e = 0; e < 4; ++e) {
+              const int at = 8 * j + e;
+              const bool seen = (at < lim) & ((at < cached) | ((first[e] <= x.number) &
+                                                               (x.number <= last[e])));
+              const int i = 4 * (j & 3) + e;
+              s[j >> 2][i] = seen ? s[j >> 2][i] : -INFINITY;
+              any |= seen;
+            }
           }
         }
       }
@@ -740,8 +755,8 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
     __syncthreads();
   };
   for (int t = 0; t < tiles; t += 2) {
-    step(t, s_k0, s_v0, s_k1, s_v1);
-    if (t + 1 < tiles) step(t + 1, s_k1, s_v1, s_k0, s_v0);
+    step(t, s_k0, s_v0, s_n0, s_k1, s_v1, s_n1);
+    if (t + 1 < tiles) step(t + 1, s_k1, s_v1, s_n1, s_k0, s_v0, s_n0);
   }
   if (32 * wv >= it.rows) return;
   l += __shfl_xor(l, 32, 64);
@@ -799,6 +814,7 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   // (buffers by name: reads of one are seen not to meet the loads into the other)
   __shared__ u32x4 s_k0[kTileStep * D / 8], s_k1[kTileStep * D / 8];
   __shared__ u32x4 s_v0[kTileStep * D / 8], s_v1[kTileStep * D / 8];
+  __shared__ i32x4 s_n0[TREE ? 32 : 1], s_n1[TREE ? 32 : 1];
   __shared__ FewShared sh;
   static_assert(sizeof(s_k0) == 2 * kFew * D * sizeof(float), "two wavefronts' outputs");
   const uint32_t turn = blockIdx.x >> 3, in = blockIdx.x & 7;
@@ -818,9 +834,11 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   const Item it = tile ? a.tile[item]
                        : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
   if (tile && it.gathered)
-    tile_item<Ty, D, true, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
+    tile_item<Ty, D, true, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1,
+                                reinterpret_cast<int*>(s_n0), reinterpret_cast<int*>(s_n1));
   else if (tile)
-    tile_item<Ty, D, false, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1);
+    tile_item<Ty, D, false, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1,
+                                reinterpret_cast<int*>(s_n0), reinterpret_cast<int*>(s_n1));
   else
     few_item<Ty, D, true, TREE>(a, it, kvh, sh, reinterpret_cast<f32x4*>(s_k0),
                           reinterpret_cast<f32x4*>(s_k1));
