@@ -833,7 +833,8 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   if (item >= (uint32_t)(tile ? a.head->tiles : all_few)) return;
   const Item it = tile ? a.tile[item]
                        : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
-  if (tile && it.gathered)
+  // (attn_paged keeps two values over every prefix)
+  if (tile && (TREE ? it.gathered == 1 : it.gathered != 0))
     tile_item<Ty, D, true, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1,
                                 reinterpret_cast<int*>(s_n0), reinterpret_cast<int*>(s_n1));
   else if (tile)
@@ -1023,7 +1024,7 @@ plora_status launch(const AttnArgs& a, const Bounds& b, hipStream_t stream) {
     hipLaunchKernelGGL((merge_kernel<Ty, D, true>), dim3(a.T, (heads + rows - 1) / rows),
                        dim3(kNT), 0, stream, a, rows);
   } else {
-    const int per = a.T < 512 ? kWaves * rows : heads;
+    const int per = a.T < kMergeTokens ? kWaves * rows : heads;
     hipLaunchKernelGGL((merge_kernel<Ty, D, false>),
                        dim3(std::min(a.T, kMergeTokens), (heads + per - 1) / per), dim3(kNT), 0,
                        stream, a, per);
