@@ -143,8 +143,10 @@ template <bool TREE>
 __device__ __forceinline__ NewKeys new_keys(const AttnArgs& a, const Item& it) {
   NewKeys x{INT32_MAX, 0};
   if constexpr (TREE) {
-    if (!it.gathered && a.tree[it.req].x) {
-      x.past = uniform(a.pos[it.tok]);
+    // (asked for together)
+    const int kind = a.tree[max(it.req, 0)].x, past = a.pos[it.gathered ? 0 : it.tok];
+    if (!it.gathered && uniform(kind)) {
+      x.past = uniform(past);
       x.shift = x.past - it.tok;
     }
   }
