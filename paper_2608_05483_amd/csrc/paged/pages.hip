@@ -123,120 +123,166 @@ __device__ __forceinline__ int block_sum(int x, int* red, int& total) {
 // One work group.  The entries that old requests drop, 1024 requests and 1024 entries
 // at a time: of those whose page nobody holds (its count is below 0) the lowest request
 // puts its mark there, and the marked ones go before the list's head, from the last to
-// the first.  Then the new requests' partly filled pages: how many hold a page so and
-// which is the last of them are known after one pass, so each can tell whether it has
-// to take a page of its own; a scan numbers those that do.
-// Bound by latency: dependent loads and barriers.
+// the first.  Then the new requests' partly filled pages that others hold too: how many
+// hold a page so and which is the last of them are known after one pass, so each can
+// tell whether it has to take a page of its own; a scan numbers those that do.
+// Bound by latency, dependent loads and barriers: what there is nothing of is left out,
+// and where all fits the threads (the usual case) entries stay in their registers.
 __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
   __shared__ int s_first[kFT], s_from[kFT];
   __shared__ int red[kFW];
   constexpr int kMark = INT32_MIN / 2;   // (a request's number is added)
   const int tid = threadIdx.x;
-  const int head = *a.free_head;
-  const bool list = head >= 0 && head <= a.n_free;
-  int room = list ? head : 0, freed = 0;
   const int chunks = (a.old_batch + kFT - 1) / kFT;
-  // visits entry after entry: f(request, page or -1, its turn)
-  const auto chunk = [&](int c, auto&& f, bool back) {
-    const int b0 = c * kFT, m = min(kFT, a.old_batch - b0);
-    const int2 d = tid < m ? a.drop[b0 + tid] : int2{0, 0};
+  const int32_t head = *a.free_head;
+  // (asked for beside the drops)
+  int part0 = tid < a.new_batch ? a.part[tid] : -1;
+  const int n0 = tid < a.new_batch ? a.new_len[tid] : 0;
+  // a chunk's entries: s_first, s_from
+  const auto open = [&](int c) {
+    const int b = c * kFT + tid;
+    const int2 d = b < a.old_batch ? a.drop[b] : int2{0, 0};
     int total;
-    s_first[tid] = block_sum(d.y, red, total);
+    const int at = block_sum(d.y, red, total);
+    s_first[tid] = at;
     s_from[tid] = d.x;
     __syncthreads();
-    const int turns = (total + kFT - 1) / kFT;
-    for (int t = 0; t < turns; ++t) {
-      const int e = (back ? turns - 1 - t : t) * kFT + tid;
-      int b = -1, page = -1;
-      if (e < total) {
-        int lo = 0, hi = m;              // the last request that starts at or before e
-        while (hi - lo > 1) {
-          const int mid = (lo + hi) >> 1;
-          if (s_first[mid] <= e) lo = mid;
-          else hi = mid;
-        }
-        b = b0 + lo;
-        page = a.old_table[(int64_t)b * a.old_max + s_from[lo] + e - s_first[lo]];
-        if (!in_pool(a, page)) page = -1;
-      }
-      f(b, page);
-    }
-    __syncthreads();
+    return total;
   };
-  for (int c = 0; c < chunks; ++c)
-    chunk(c, [&](int b, int page) {
-      if (page >= 0 && now(&a.shares[page]) < 0) atomicMin(&a.shares[page], kMark + b);
-    }, false);
-  for (int c = chunks - 1; c >= 0; --c)
-    chunk(c, [&](int b, int page) {
-      const bool mine = page >= 0 && now(&a.shares[page]) == kMark + b;
-      int total;
-      const int before = block_sum(mine, red, total);
-      // (the last of this turn is put right before the head)
-      const int at = room - total + before;
-      if (mine) {
-        a.shares[page] = 0;
-        if (at >= 0) a.free_pages[at] = page;
-      }
-      room -= total;
-      freed += total;
-    }, true);
-  const int put = min(freed, list ? head : 0), top = head - put;
-  const int avail = list ? a.n_free - top : 0;
-  __threadfence();
-  __syncthreads();
-  // partly filled pages
-  for (int i = tid; i < a.new_batch; i += kFT) {
-    const int page = a.part[i];
-    if (page >= 0) atomicAdd(&a.last[page].x, 1), atomicMax(&a.last[page].y, i);
-  }
-  __syncthreads();
-  int taken = 0;
-  for (int i0 = 0; i0 < a.new_batch; i0 += kFT) {
-    const int i = i0 + tid;
-    const int page = i < a.new_batch ? a.part[i] : -1;
-    bool own = false;
-    if (page >= 0) {
-      const int holders = now(&a.shares[page]) + 1;
-      own = holders > 1 && (now(&a.last[page].x) != holders || now(&a.last[page].y) != i);
+  const auto entry = [&](int c, int e, int total, int& b, int& page) {
+    b = page = -1;
+    if (e >= total) return;
+    int lo = 0, hi = min(kFT, a.old_batch - c * kFT);
+    while (hi - lo > 1) {                // the last request that starts at or before e
+      const int mid = (lo + hi) >> 1;
+      if (s_first[mid] <= e) lo = mid;
+      else hi = mid;
     }
+    b = c * kFT + lo;
+    page = a.old_table[(int64_t)b * a.old_max + s_from[lo] + e - s_first[lo]];
+    if (!in_pool(a, page)) page = -1;
+  };
+  const auto mark = [&](int b, int page) {
+    if (page >= 0 && now(&a.shares[page]) < 0) atomicMin(&a.shares[page], kMark + b);
+  };
+  const bool list = head >= 0 && head <= a.n_free;
+  int room = list ? head : 0, freed = 0;
+  const auto put = [&](int b, int page) {
+    const bool mine = page >= 0 && now(&a.shares[page]) == kMark + b;
     int total;
-    const int at = taken + block_sum(own, red, total);
-    taken += total;
-    if (own) {
-      const int n = a.new_len[i], S1 = (1 << a.log_page) - 1;
-      if (at < avail) {
-        const int fresh = now(&a.free_pages[top + at]);
-        a.new_table[(int64_t)i * a.new_max + (n >> a.log_page)] = fresh;
-        a.copies[3 * at] = page;
-        a.copies[3 * at + 1] = fresh;
-        a.copies[3 * at + 2] = n & S1;
-      } else {
-        a.new_len[i] = n & ~S1;
+    const int before = block_sum(mine, red, total);
+    const int at = room - total + before;
+    if (mine) {
+      a.shares[page] = 0;
+      if (at >= 0) a.free_pages[at] = page;
+    }
+    room -= total;
+    freed += total;
+  };
+  if (chunks == 1) {
+    const int total = open(0);
+    if (total > 0 && total <= kFT) {
+      int b, page;
+      entry(0, tid, total, b, page);
+      mark(b, page);
+      __syncthreads();
+      put(b, page);
+    } else if (total > 0) {
+      const int turns = (total + kFT - 1) / kFT;
+      for (int t = 0; t < turns; ++t) {
+        int b, page;
+        entry(0, t * kFT + tid, total, b, page);
+        mark(b, page);
+      }
+      __syncthreads();
+      for (int t = turns - 1; t >= 0; --t) {
+        int b, page;
+        entry(0, t * kFT + tid, total, b, page);
+        put(b, page);
       }
     }
+  } else {
+    for (int c = 0; c < chunks; ++c) {
+      const int total = open(c);
+      for (int e = tid; e < total; e += kFT) {
+        int b, page;
+        entry(c, e, total, b, page);
+        mark(b, page);
+      }
+      __syncthreads();
+    }
+    for (int c = chunks - 1; c >= 0; --c) {
+      const int total = open(c);
+      for (int t = (total + kFT - 1) / kFT - 1; t >= 0; --t) {
+        int b, page;
+        entry(c, t * kFT + tid, total, b, page);
+        put(b, page);
+      }
+      __syncthreads();
+    }
   }
-  // (counts change once nobody asks for them any more)
-  __syncthreads();
-  const int given = min(taken, max(avail, 0));
+  const int back = min(freed, list ? head : 0), top = head - back;
+  const int avail = list ? a.n_free - top : 0;
+  // partly filled pages with other holders, and those who hold them so
+  bool some = false;
   for (int i = tid; i < a.new_batch; i += kFT) {
-    const int page = a.part[i];
-    if (page >= 0) {
-      const int2 l = {now(&a.last[page].x), now(&a.last[page].y)};
-      // all that held it so took pages of their own, but the last if nobody else holds it
-      if (l.y == i) {
+    const int page = i == tid ? part0 : a.part[i];
+    if (page >= 0 && now(&a.shares[page]) > 0) {
+      atomicAdd(&a.last[page].x, 1);
+      atomicMax(&a.last[page].y, i);
+      some = true;
+    }
+  }
+  int taken = 0;
+  // (and what has been put into the list is there for all)
+  __threadfence();
+  if (__syncthreads_or(some)) {
+    for (int i0 = 0; i0 < a.new_batch; i0 += kFT) {
+      const int i = i0 + tid;
+      const int page = i >= a.new_batch ? -1 : i == tid ? part0 : a.part[i];
+      bool own = false;
+      if (page >= 0) {
         const int holders = now(&a.shares[page]) + 1;
-        if (holders > 1) a.shares[page] = holders - 1 - (l.x == holders ? l.x - 1 : l.x);
+        const int how_many = now(&a.last[page].x), last = now(&a.last[page].y);
+        own = holders > 1 && (how_many != holders || last != i);
+      }
+      int total;
+      const int at = taken + block_sum(own, red, total);
+      taken += total;
+      if (own) {
+        const int n = i == tid ? n0 : a.new_len[i], S1 = (1 << a.log_page) - 1;
+        if (at < avail) {
+          const int fresh = now(&a.free_pages[top + at]);
+          a.new_table[(int64_t)i * a.new_max + (n >> a.log_page)] = fresh;
+          a.copies[3 * at] = page;
+          a.copies[3 * at + 1] = fresh;
+          a.copies[3 * at + 2] = n & S1;
+        } else {
+          a.new_len[i] = n & ~S1;
+        }
       }
     }
-    if (i >= given) a.copies[3 * i] = a.copies[3 * i + 1] = a.copies[3 * i + 2] = -1;
+    // (counts change once nobody asks for them any more)
+    __syncthreads();
+    for (int i = tid; i < a.new_batch; i += kFT) {
+      const int page = i == tid ? part0 : a.part[i];
+      if (page >= 0 && now(&a.last[page].y) == i) {
+        // all that held it so took pages of their own, but the last if nobody else
+        // holds it
+        const int holders = now(&a.shares[page]) + 1, how_many = now(&a.last[page].x);
+        if (holders > 1) a.shares[page] = holders - 1 - how_many + (how_many == holders);
+      }
+    }
   }
+  const int given = min(taken, max(avail, 0));
+  for (int i = given + tid; i < a.new_batch; i += kFT)
+    a.copies[3 * i] = a.copies[3 * i + 1] = a.copies[3 * i + 2] = -1;
   if (tid == 0) {
     *a.free_next = top + given;
-    a.meta[0] = put;
+    a.meta[0] = back;
     a.meta[1] = given;
     a.meta[2] = taken - given;
-    a.meta[3] = freed - put;
+    a.meta[3] = freed - back;
   }
   if (tid >= 4 && tid < 8) a.meta[tid] = 0;
 }
@@ -249,56 +295,103 @@ struct MoveArgs {
   int32_t n_pages, log_page, kv_heads, units;       // units of a row
 };
 
-template <class U>
-__device__ __forceinline__ U* at(const MoveArgs& a, uint8_t* pool, int64_t page, int key) {
-  return reinterpret_cast<U*>(pool + page * a.page_stride + key * a.token_stride);
-}
-
 // A work group copies a page's keys in k or v of a layer: neighbouring threads take
-// neighbouring units of a row, then the rows of a head, then the heads.  Bound by
+// neighbouring units of a row, kAtOnce rows of a thread on their way together.  Bound by
 // reading and writing.
+constexpr int kAtOnce = 8;
 template <class U>
 __global__ __launch_bounds__(kNT) void copy_kernel(MoveArgs a, const int32_t* copies, int32_t cap,
                                                    const int32_t* n_copies) {
   const int e = blockIdx.x;
-  if (e >= min(*n_copies, cap)) return;
-  const int from = copies[3 * e], to = copies[3 * e + 1];
-  const int keys = min(copies[3 * e + 2], 1 << a.log_page);
+  const int n = *n_copies, from = copies[3 * e], to = copies[3 * e + 1], some = copies[3 * e + 2];
+  if (e >= min(n, cap)) return;
+  const int keys = min(some, 1 << a.log_page);
   if (from < 0 || from >= a.n_pages || to < 0 || to >= a.n_pages || keys <= 0) return;
   uint8_t* pool = a.pool[2 * blockIdx.y + blockIdx.z];
-  const U* x = at<U>(a, pool, from, 0);
-  U* y = at<U>(a, pool, to, 0);
-  const int per_head = keys * a.units, n = per_head * a.kv_heads;
-  for (int i = threadIdx.x; i < n; i += kNT) {
-    const int h = i / per_head, j = i - h * per_head, key = j / a.units, u = j - key * a.units;
-    const int64_t off = h * a.head_stride + key * a.token_stride + (int64_t)u * sizeof(U);
-    *reinterpret_cast<U*>(reinterpret_cast<uint8_t*>(y) + off) =
-        *reinterpret_cast<const U*>(reinterpret_cast<const uint8_t*>(x) + off);
+  const uint8_t* x = pool + from * a.page_stride;
+  uint8_t* y = pool + to * a.page_stride;
+  const int wide = min(a.units, kNT), per = kNT / wide;    // units and rows at a time
+  const int rows = keys * a.kv_heads;
+  if ((int)threadIdx.x >= wide * per) return;
+  for (int u = threadIdx.x % wide; u < a.units; u += wide) {
+    for (int r0 = threadIdx.x / wide; r0 < rows; r0 += per * kAtOnce) {
+      U v[kAtOnce];
+      int64_t off[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const int r = min(r0 + i * per, rows - 1), h = (uint32_t)r / (uint32_t)keys;
+        off[i] = h * a.head_stride + (r - h * keys) * a.token_stride + (int64_t)u * sizeof(U);
+        v[i] = *reinterpret_cast<const U*>(x + off[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (r0 + i * per < rows) *reinterpret_cast<U*>(y + off[i]) = v[i];
+    }
   }
 }
 
 // A thread moves one unit of a head's row, in k or v of a layer, for all keys of a
-// request's path one after the other; what it moves nobody else touches, and a path's
-// numbers rise, so no key is overwritten before it is read.  Bound by latency.
+// request's path, which nobody else touches.  A lane looks up a move, 64 at once.  Up to
+// kAtOnce keys are read before they are stored where that is the same as one after the
+// other: a path's numbers are not below their places, so no key of the ones read
+// together is where an earlier one of them goes.  Bound by latency.
 template <class U>
 __global__ __launch_bounds__(kNT) void compact_kernel(MoveArgs a, const int32_t* q_start,
                                                       const int32_t* req, const int64_t* slot,
                                                       const int32_t* path, const int32_t* count,
                                                       int32_t T, int32_t parts) {
-  const int b = blockIdx.x / parts, c = (blockIdx.x % parts) * kNT + threadIdx.x;
+  const int b = blockIdx.x / parts, c = (blockIdx.x % parts) * blockDim.x + threadIdx.x;
+  const int lane = threadIdx.x & 63;
+  const int some = count[b];
   const int q0 = max(q_start[b], 0), n = min(q_start[b + 1], T) - q0;
-  if (n <= 0 || req[q0] != b || c >= a.kv_heads * a.units) return;
-  const int m = min(count[b], n), S1 = (1 << a.log_page) - 1;
+  if (n <= 0) return;
+  const int first = req[q0], m = min(some, n);
   const int64_t slots = (int64_t)a.n_pages << a.log_page;
+  const bool mine = c < a.kv_heads * a.units;
   uint8_t* pool = a.pool[2 * blockIdx.y + blockIdx.z] + (c / a.units) * a.head_stride +
                   (int64_t)(c % a.units) * sizeof(U);
-  for (int i = 0; i < m; ++i) {
-    const int j = path[q0 + i];
-    if (j == i || j < 0 || j >= n) continue;
-    const int64_t from = slot[q0 + j], to = slot[q0 + i];
-    if (from < 0 || from >= slots || to < 0 || to >= slots) continue;
-    *at<U>(a, pool, to >> a.log_page, (int)to & S1) =
-        *at<U>(a, pool, from >> a.log_page, (int)from & S1);
+  if (first != b) return;
+  for (int i0 = 0; i0 < m; i0 += 64) {
+    // this lane's move, a slot below 0 for none
+    const int i = i0 + lane;
+    int64_t from = -1, to = -1;
+    bool late = false;
+    if (i < m) {
+      const int j = path[q0 + i];
+      if (j != i && j >= 0 && j < n) {
+        from = slot[q0 + j];
+        to = slot[q0 + i];
+        if (from < 0 || from >= slots || to < 0 || to >= slots) from = -1;
+        late = j < i;
+      }
+    }
+    uint64_t todo = __ballot(from >= 0);
+    const int most = __any(late) ? 1 : kAtOnce;
+    const int64_t S1 = (1 << a.log_page) - 1;
+    const int64_t from_at = (from >> a.log_page) * a.page_stride + (from & S1) * a.token_stride;
+    const int64_t to_at = (to >> a.log_page) * a.page_stride + (to & S1) * a.token_stride;
+    const auto of = [](int64_t x, int l) {
+      return (int64_t)(uint32_t)__builtin_amdgcn_readlane((int)x, l) |
+             (int64_t)__builtin_amdgcn_readlane((int)(x >> 32), l) << 32;
+    };
+    while (todo) {
+      U v[kAtOnce];
+      int64_t y[kAtOnce];
+      int k = 0;
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q) {
+        if (q < most && todo) {
+          const int l = __builtin_ctzll(todo);
+          todo &= todo - 1;
+          y[q] = of(to_at, l);
+          if (mine) v[q] = *reinterpret_cast<const U*>(pool + of(from_at, l));
+          k = q + 1;
+        }
+      }
+#pragma unroll
+      for (int q = 0; q < kAtOnce; ++q)
+        if (q < k && mine) *reinterpret_cast<U*>(pool + y[q]) = v[q];
+    }
   }
 }
 
@@ -475,10 +568,11 @@ extern "C" plora_status plora_kv_compact(const plora_kv_cache* caches, int32_t l
     return PLORA_OK;
   if (!step->q_start || !step->req || !step->slot || !path || !count)
     return PLORA_ERR_INVALID_ARG;
-  const int parts = (a.kv_heads * a.units + kNT - 1) / kNT;
+  const int columns = a.kv_heads * a.units, threads = std::min(kNT, (columns + 63) / 64 * 64);
+  const int parts = (columns + threads - 1) / threads;
   return by_layers(caches, layers, a, bytes, [&](auto u, int n) {
-    hipLaunchKernelGGL(compact_kernel<decltype(u)>, dim3(step->batch * parts, n, 2), dim3(kNT), 0,
-                       stream, a, step->q_start, step->req, step->slot, path, count, step->T,
+    hipLaunchKernelGGL(compact_kernel<decltype(u)>, dim3(step->batch * parts, n, 2), dim3(threads),
+                       0, stream, a, step->q_start, step->req, step->slot, path, count, step->T,
                        parts);
   });
 }
