@@ -120,14 +120,17 @@ __device__ __forceinline__ int block_sum(int x, int* red, int& total) {
   return before + inc - x;
 }
 
-// One work group.  The entries that old requests drop, 1024 requests and 1024 entries
-// at a time: of those whose page nobody holds (its count is below 0) the lowest request
-// puts its mark there, and the marked ones go before the list's head, from the last to
-// the first.  Then the new requests' partly filled pages that others hold too: how many
-// hold a page so and which is the last of them are known after one pass, so each can
-// tell whether it has to take a page of its own; a scan numbers those that do.
-// Bound by latency, dependent loads and barriers: what there is nothing of is left out,
-// and where all fits the threads (the usual case) entries stay in their registers.
+// One work group.  The entries that old requests drop, of 1024 requests at a time: of
+// those whose page nobody holds (its count is below 0) the lowest request puts its mark
+// there, and the marked ones go before the list's head, from the last to the first.  Then
+// the new requests' partly filled pages that others hold too: how many hold a page so and
+// which is the last of them are known after one pass, so each can tell whether it has to
+// take a page of its own; a scan numbers those that do.
+// Bound by latency, dependent loads and barriers: what there is nothing of is left out, a
+// thread asks for kEach entries in a row together, and what it has found of them, and of
+// its new request, stays in registers where all fits (the usual case).
+constexpr int kEach = 8;
+constexpr int kTurn = kFT * kEach;
 __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
   __shared__ int s_first[kFT], s_from[kFT];
   __shared__ int red[kFW];
@@ -136,9 +139,11 @@ __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
   const int chunks = (a.old_batch + kFT - 1) / kFT;
   const int32_t head = *a.free_head;
   // (asked for beside the drops)
-  int part0 = tid < a.new_batch ? a.part[tid] : -1;
+  const int part0 = tid < a.new_batch ? a.part[tid] : -1;
   const int n0 = tid < a.new_batch ? a.new_len[tid] : 0;
-  // a chunk's entries: s_first, s_from
+  const bool list = head >= 0 && head <= a.n_free;
+  int room = list ? head : 0, freed = 0;
+  // a chunk's requests: where their entries begin in order, and in their rows
   const auto open = [&](int c) {
     const int b = c * kFT + tid;
     const int2 d = b < a.old_batch ? a.drop[b] : int2{0, 0};
@@ -149,77 +154,72 @@ __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
     __syncthreads();
     return total;
   };
-  const auto entry = [&](int c, int e, int total, int& b, int& page) {
-    b = page = -1;
-    if (e >= total) return;
-    int lo = 0, hi = min(kFT, a.old_batch - c * kFT);
-    while (hi - lo > 1) {                // the last request that starts at or before e
+  // this thread's entries of a turn: their requests and pages (-1: none)
+  struct Entries {
+    int b[kEach], page[kEach];
+  } x;
+  const auto get = [&](int c, int turn, int total) {
+    const int e0 = turn * kTurn + tid * kEach, m = min(kFT, a.old_batch - c * kFT);
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) x.b[k] = x.page[k] = -1;
+    if (e0 >= total) return;
+    int lo = 0, hi = m;
+    while (hi - lo > 1) {                // the last request that starts at or before e0
       const int mid = (lo + hi) >> 1;
-      if (s_first[mid] <= e) lo = mid;
+      if (s_first[mid] <= e0) lo = mid;
       else hi = mid;
     }
-    b = c * kFT + lo;
-    page = a.old_table[(int64_t)b * a.old_max + s_from[lo] + e - s_first[lo]];
-    if (!in_pool(a, page)) page = -1;
-  };
-  const auto mark = [&](int b, int page) {
-    if (page >= 0 && now(&a.shares[page]) < 0) atomicMin(&a.shares[page], kMark + b);
-  };
-  const bool list = head >= 0 && head <= a.n_free;
-  int room = list ? head : 0, freed = 0;
-  const auto put = [&](int b, int page) {
-    const bool mine = page >= 0 && now(&a.shares[page]) == kMark + b;
-    int total;
-    const int before = block_sum(mine, red, total);
-    const int at = room - total + before;
-    if (mine) {
-      a.shares[page] = 0;
-      if (at >= 0) a.free_pages[at] = page;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      if (e0 + k >= total) break;
+      while (lo + 1 < m && s_first[lo + 1] <= e0 + k) ++lo;
+      x.b[k] = c * kFT + lo;
+      x.page[k] = a.old_table[(int64_t)x.b[k] * a.old_max + s_from[lo] + e0 + k - s_first[lo]];
     }
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (!in_pool(a, x.page[k])) x.page[k] = -1;
+  };
+  const auto mark = [&]() {
+    int n[kEach];
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) n[k] = x.page[k] >= 0 ? now(&a.shares[x.page[k]]) : 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (n[k] < 0) atomicMin(&a.shares[x.page[k]], kMark + x.b[k]);
+  };
+  const auto put = [&]() {
+    int n[kEach], mine = 0, total;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) n[k] = x.page[k] >= 0 ? now(&a.shares[x.page[k]]) : 0;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) mine += x.page[k] >= 0 && n[k] == kMark + x.b[k];
+    // (the last of this turn is put right before the head)
+    int at = block_sum(mine, red, total);
+    at += room - total;
+#pragma unroll
+    for (int k = 0; k < kEach; ++k)
+      if (x.page[k] >= 0 && n[k] == kMark + x.b[k]) {
+        a.shares[x.page[k]] = 0;
+        if (at >= 0) a.free_pages[at] = x.page[k];
+        ++at;
+      }
     room -= total;
     freed += total;
   };
-  if (chunks == 1) {
-    const int total = open(0);
-    if (total > 0 && total <= kFT) {
-      int b, page;
-      entry(0, tid, total, b, page);
-      mark(b, page);
-      __syncthreads();
-      put(b, page);
-    } else if (total > 0) {
-      const int turns = (total + kFT - 1) / kFT;
-      for (int t = 0; t < turns; ++t) {
-        int b, page;
-        entry(0, t * kFT + tid, total, b, page);
-        mark(b, page);
-      }
-      __syncthreads();
-      for (int t = turns - 1; t >= 0; --t) {
-        int b, page;
-        entry(0, t * kFT + tid, total, b, page);
-        put(b, page);
-      }
+  int total = 0;
+  for (int c = 0; c < chunks; ++c) {
+    total = open(c);
+    for (int t = 0; t * kTurn < total; ++t) get(c, t, total), mark();
+    __syncthreads();
+  }
+  for (int c = chunks - 1; c >= 0; --c) {
+    if (c < chunks - 1) total = open(c);
+    for (int t = (total + kTurn - 1) / kTurn - 1; t >= 0; --t) {
+      if (chunks > 1 || total > kTurn) get(c, t, total);
+      put();
     }
-  } else {
-    for (int c = 0; c < chunks; ++c) {
-      const int total = open(c);
-      for (int e = tid; e < total; e += kFT) {
-        int b, page;
-        entry(c, e, total, b, page);
-        mark(b, page);
-      }
-      __syncthreads();
-    }
-    for (int c = chunks - 1; c >= 0; --c) {
-      const int total = open(c);
-      for (int t = (total + kFT - 1) / kFT - 1; t >= 0; --t) {
-        int b, page;
-        entry(c, t * kFT + tid, total, b, page);
-        put(b, page);
-      }
-      __syncthreads();
-    }
+    __syncthreads();
   }
   const int back = min(freed, list ? head : 0), top = head - back;
   const int avail = list ? a.n_free - top : 0;
@@ -234,21 +234,24 @@ __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
     }
   }
   int taken = 0;
-  // (and what has been put into the list is there for all)
-  __threadfence();
+  // what a request's page was found to be
+  int holders = 0, how_many = 0, last = -1;
+  const auto look = [&](int page) {
+    holders = how_many = 0, last = -1;
+    if (page < 0) return;
+    holders = now(&a.shares[page]) + 1;
+    how_many = now(&a.last[page].x), last = now(&a.last[page].y);
+  };
+  // (and what has been put into the list is there for the work group)
   if (__syncthreads_or(some)) {
     for (int i0 = 0; i0 < a.new_batch; i0 += kFT) {
       const int i = i0 + tid;
       const int page = i >= a.new_batch ? -1 : i == tid ? part0 : a.part[i];
-      bool own = false;
-      if (page >= 0) {
-        const int holders = now(&a.shares[page]) + 1;
-        const int how_many = now(&a.last[page].x), last = now(&a.last[page].y);
-        own = holders > 1 && (how_many != holders || last != i);
-      }
-      int total;
-      const int at = taken + block_sum(own, red, total);
-      taken += total;
+      look(page);
+      const bool own = holders > 1 && (how_many != holders || last != i);
+      int more;
+      const int at = taken + block_sum(own, red, more);
+      taken += more;
       if (own) {
         const int n = i == tid ? n0 : a.new_len[i], S1 = (1 << a.log_page) - 1;
         if (at < avail) {
@@ -262,16 +265,14 @@ __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
         }
       }
     }
-    // (counts change once nobody asks for them any more)
+    // counts change once nobody asks for them any more: all that held a page so took
+    // pages of their own, but the last if nobody else holds it
     __syncthreads();
     for (int i = tid; i < a.new_batch; i += kFT) {
       const int page = i == tid ? part0 : a.part[i];
-      if (page >= 0 && now(&a.last[page].y) == i) {
-        // all that held it so took pages of their own, but the last if nobody else
-        // holds it
-        const int holders = now(&a.shares[page]) + 1, how_many = now(&a.last[page].x);
-        if (holders > 1) a.shares[page] = holders - 1 - how_many + (how_many == holders);
-      }
+      if (a.new_batch > kFT) look(page);
+      if (holders > 1 && last == i)
+        a.shares[page] = holders - 1 - how_many + (how_many == holders);
     }
   }
   const int given = min(taken, max(avail, 0));
