@@ -41,24 +41,28 @@ __device__ __forceinline__ int now(const int32_t* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// The lowest of the work group's values.
+// The lowest of a team's values: a wavefront's, or (red) a work group's of kNT threads.
+template <int NT>
 __device__ __forceinline__ int lowest(int x, int* red) {
 #pragma unroll
   for (int d = 32; d; d >>= 1) x = min(x, __shfl_xor(x, d, 64));
-  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
-  __syncthreads();
+  if constexpr (NT > 64) {
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
+    __syncthreads();
 #pragma unroll
-  for (int w = 0; w < kNT / 64; ++w) x = min(x, red[w]);
+    for (int w = 0; w < NT / 64; ++w) x = min(x, red[w]);
+  }
   return x;
 }
 
-// A work group for each new and each old request.  An old request's holds pass to the
-// first new one that continues it, so only what changes is counted: that one's shorter
-// tail and the pages of requests that none continues are dropped, the other
-// continuations hold theirs in addition.  Sums of whole numbers, in any order.
-__global__ __launch_bounds__(kNT) void remap_rows_kernel(RemapArgs a) {
-  __shared__ int red[kNT / 64];
-  const int tid = threadIdx.x, i = blockIdx.x;
+// New request i, or old request i - new_batch, by a team of NT threads.  An old
+// request's holds pass to the first new one that continues it, so only what changes is
+// counted: that one's shorter tail and the pages of requests that none continues are
+// dropped, the other continuations hold theirs in addition.  Sums of whole numbers, in
+// any order.
+template <int NT>
+__device__ __forceinline__ void remap_row(const RemapArgs& a, int i, int* red) {
+  const int tid = threadIdx.x % NT;
   if (i < a.new_batch) {
     const int b = a.src[i], n = new_length(a, i, b), pages = pages_of(a, n);
     if (tid == 0) {
@@ -67,12 +71,12 @@ __global__ __launch_bounds__(kNT) void remap_rows_kernel(RemapArgs a) {
     }
     if (pages == 0) return;
     int first = i;
-    for (int j = tid; j < i; j += kNT)
+    for (int j = tid; j < i; j += NT)
       if (a.src[j] == b) first = min(first, j);
-    first = lowest(first, red);
+    first = lowest<NT>(first, red);
     const int32_t* from = a.old_table + (int64_t)b * a.old_max;
     int32_t* to = a.new_table + (int64_t)i * a.new_max;
-    for (int j = tid; j < pages; j += kNT) {
+    for (int j = tid; j < pages; j += NT) {
       const int page = from[j];
       const bool held = in_pool(a, page);
       to[j] = page;
@@ -86,18 +90,23 @@ __global__ __launch_bounds__(kNT) void remap_rows_kernel(RemapArgs a) {
   } else {
     const int b = i - a.new_batch;
     int first = a.new_batch;
-    for (int j = tid; j < a.new_batch; j += kNT)
+    for (int j = tid; j < a.new_batch; j += NT)
       if (a.src[j] == b) first = min(first, j);
-    first = lowest(first, red);
+    first = lowest<NT>(first, red);
     const int kept = first < a.new_batch ? pages_of(a, new_length(a, first, b)) : 0;
     const int held = pages_of(a, old_length(a, b));
     if (tid == 0) a.drop[b] = int2{kept, held - kept};
     const int32_t* from = a.old_table + (int64_t)b * a.old_max;
-    for (int j = kept + tid; j < held; j += kNT) {
+    for (int j = kept + tid; j < held; j += NT) {
       const int page = from[j];
       if (in_pool(a, page)) atomicAdd(&a.shares[page], -1);
     }
   }
+}
+
+__global__ __launch_bounds__(kNT) void remap_rows_kernel(RemapArgs a) {
+  __shared__ int red[kNT / 64];
+  remap_row<kNT>(a, blockIdx.x, red);
 }
 
 constexpr int kFT = 1024;                // threads, and requests looked at together
@@ -129,8 +138,10 @@ __device__ __forceinline__ int block_sum(int x, int* red, int& total) {
 // Bound by latency, dependent loads and barriers: what there is nothing of is left out, a
 // thread asks for kEach entries in a row together, and what it has found of them, and of
 // its new request, stays in registers where all fits (the usual case).
+// ROWS: the requests as well, a wavefront each.
 constexpr int kEach = 8;
 constexpr int kTurn = kFT * kEach;
+template <bool ROWS>
 __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
   __shared__ int s_first[kFT], s_from[kFT];
   __shared__ int red[kFW];
@@ -138,6 +149,10 @@ __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
   const int tid = threadIdx.x;
   const int chunks = (a.old_batch + kFT - 1) / kFT;
   const int32_t head = *a.free_head;
+  if constexpr (ROWS) {
+    for (int i = tid >> 6; i < a.new_batch + a.old_batch; i += kFW) remap_row<64>(a, i, nullptr);
+    __syncthreads();
+  }
   // (asked for beside the drops)
   const int part0 = tid < a.new_batch ? a.part[tid] : -1;
   const int n0 = tid < a.new_batch ? a.new_len[tid] : 0;
@@ -454,6 +469,16 @@ plora_status by_layers(const plora_kv_cache* c, int32_t layers, MoveArgs& a, int
   return PLORA_OK;
 }
 
+// Whether the one work group does everything: few requests of both batches, and few
+// entries at most.  (Two remaps, there and back, in a graph, so and in two launches each:
+// 9 requests of 32 pages 13.5 us and 17.0, of 251 pages 16.0 and 17.9, of 938 pages 30 and
+// 24; 20 of 63 pages 16.5 and 18.5; 40 of 63 19.2 and 18.7; 60 of 63 24.0 and 19.5.)
+constexpr int kInOneRows = 32, kInOneEntries = 4096;
+bool remap_in_one(const RemapArgs& a) {
+  return a.old_batch + a.new_batch <= kInOneRows &&
+         (int64_t)(a.old_batch + a.new_batch) * std::max(a.old_max, a.new_max) <= kInOneEntries;
+}
+
 struct RemapWs {
   size_t drop, bytes;
 };
@@ -524,12 +549,14 @@ extern "C" plora_status plora_kv_remap(const plora_kv_batch* old_batch, const in
   a.drop = reinterpret_cast<int2*>(p + w.drop);
   a.last = reinterpret_cast<int2*>(pool->scratch);
   clear_error();
-  if (o.batch + n.batch > 0) {
-    hipLaunchKernelGGL(remap_rows_kernel, dim3(o.batch + n.batch), dim3(kNT), 0, stream, a);
-    const plora_status st = launch_status();
-    if (st != PLORA_OK) return st;
+  if (remap_in_one(a)) {
+    hipLaunchKernelGGL(remap_finish_kernel<true>, dim3(1), dim3(kFT), 0, stream, a);
+    return launch_status();
   }
-  hipLaunchKernelGGL(remap_finish_kernel, dim3(1), dim3(kFT), 0, stream, a);
+  hipLaunchKernelGGL(remap_rows_kernel, dim3(o.batch + n.batch), dim3(kNT), 0, stream, a);
+  const plora_status st = launch_status();
+  if (st != PLORA_OK) return st;
+  hipLaunchKernelGGL(remap_finish_kernel<false>, dim3(1), dim3(kFT), 0, stream, a);
   return launch_status();
 }
 
