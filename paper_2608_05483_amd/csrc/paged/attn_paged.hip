@@ -37,13 +37,23 @@ struct AttnArgs {
   const PlanHeader* head;
   const Item *few, *last_few, *tile;
   const ReqInfo* info;
-  int32_t batch, T, r, kv_heads;
+  int32_t batch, T, r, kv_heads, tile_cap;
   float c;                  // |scale| log2(e)
   uint32_t flip;            // sign bits for q where scale < 0
   uint16_t* out;
   float *pm, *pl, *po;      // partials: [row][kv_heads], [row][kv_heads][D]
   const int2 *span, *tree;  // trees: intervals by token, kinds by request
 };
+
+// The launch's arguments, read again: what is used only behind an item's loop would
+// otherwise be held in scalar registers through it, which there are too few of.
+__device__ __forceinline__ AttnArgs args_again() {
+  auto p = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(p));
+  AttnArgs a;
+  __builtin_memcpy(&a, (const void*)p, sizeof(a));
+  return a;
+}
 
 __device__ __forceinline__ f32x4 mfma16(Bf16, u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a),
@@ -549,6 +559,11 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
   if (it.rows <= 0) return;
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   const int n = lane & 31, h = lane >> 5;
+  // (the first pages, asked for beside the rows)
+  const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
+  int page = 0, at_lo = 0, at_hi = 0, bytes = 0;
+  const auto ask = [&](int k0) { page = row[min(k0 + 16 * lane, it.hi - 1) >> a.log_page]; };
+  ask(it.lo);
   const Row x = query_row<TREE>(a, it, kvh, 32 * wv + n);
   const NewKeys fresh = new_keys<TREE>(a, it);
   bool any = x.limit > it.lo && (!TREE || it.lo < fresh.past);
@@ -575,14 +590,11 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) end = max(end, s_most[w]);
   end = uniform(end);
-  const int32_t* row = a.table + (int64_t)it.req * a.max_pages;
   const int tiles = (end - it.lo + kTileStep - 1) / kTileStep;
   const int my = (most - it.lo + kTileStep - 1) / kTileStep;
 
   // Where 16 keys lie is found out for 64 times 16 keys at once, a lane each
   // (their pages are asked for 16 steps ahead), and read from the lanes.
-  int page = 0, at_lo = 0, at_hi = 0, bytes = 0;
-  const auto ask = [&](int k0) { page = row[min(k0 + 16 * lane, end - 1) >> a.log_page]; };
   const auto locate = [&](int k0) {
     const int key = k0 + 16 * lane;
     const bool ok = page >= 0 && page < a.n_pages && key < end;
@@ -641,7 +653,6 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 #pragma unroll
     for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
   if (tiles > 0) {
-    ask(it.lo);
     fetch(0, s_k0, s_v0, s_n0);
     loads_done();
   }
@@ -761,6 +772,7 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
     if (t + 1 < tiles) step(t + 1, s_k1, s_v1, s_n1, s_k0, s_v0, s_n0);
   }
   if (32 * wv >= it.rows) return;
+  const AttnArgs z = args_again();
   l += __shfl_xor(l, 32, 64);
   if constexpr (TREE) {
     const int other = __shfl_xor((int)any, 32, 64);   // (by all lanes)
@@ -778,8 +790,8 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
   bad = (bad | bad >> 32) & 0xffffffffu;
   if (mine && !(bad >> n & 1)) {
     const float inv = any ? 1.f / l : 0.f;
-    const int64_t at = ((int64_t)it.part + 32 * wv + n) * a.kv_heads + kvh;
-    if (it.part >= 0 && h == 0) a.pm[at] = m - Ty::kTileLift, a.pl[at] = l;
+    const int64_t at = ((int64_t)it.part + 32 * wv + n) * z.kv_heads + kvh;
+    if (it.part >= 0 && h == 0) z.pm[at] = m - Ty::kTileLift, z.pl[at] = l;
 #pragma unroll
     for (int d = 0; d < kV; ++d)
 #pragma unroll
@@ -787,15 +799,15 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
         const int e = 32 * d + 2 * i + 4 * h;
         const float o[4] = {acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
         if (it.part < 0)
-          store_out<Ty, 4>(a.out + x.token * a.out_token + x.head * a.out_head + e, o, inv);
+          store_out<Ty, 4>(z.out + x.token * z.out_token + x.head * z.out_head + e, o, inv);
         else
-          store_part<4>(a.po + at * D + e, o);
+          store_part<4>(z.po + at * D + e, o);
       }
   }
   while (bad) {
     const int i = __builtin_ctzll(bad);
     bad &= bad - 1;
-    careful_row<Ty, D, TREE>(a, it, kvh, 32 * wv + i);
+    careful_row<Ty, D, TREE>(z, it, kvh, 32 * wv + i);
   }
 }
 
@@ -820,6 +832,8 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   __shared__ FewShared sh;
   static_assert(sizeof(s_k0) == 2 * kFew * D * sizeof(float), "two wavefronts' outputs");
   const uint32_t turn = blockIdx.x >> 3, in = blockIdx.x & 7;
+  // (the item of a step without few items, read beside their number)
+  const Item first = a.tile[min(blockIdx.x / (uint32_t)a.kv_heads, (uint32_t)a.tile_cap - 1)];
   const int few = a.head->few, all_few = few + a.head->later;
   const uint32_t tiles = ((uint32_t)a.head->tiles * a.kv_heads + 7) / 8;
   const uint32_t fews = ((uint32_t)all_few * a.kv_heads + 7) / 8;
@@ -833,8 +847,9 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   const int kvh = index % a.kv_heads;
   // (the work groups behind the last item would pass the lists' ends)
   if (item >= (uint32_t)(tile ? a.head->tiles : all_few)) return;
-  const Item it = tile ? a.tile[item]
-                       : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
+  Item it = first;
+  if (all_few != 0)
+    it = tile ? a.tile[item] : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
   // (attn_paged keeps two values over every prefix)
   if (tile && (TREE ? it.gathered == 1 : it.gathered != 0))
     tile_item<Ty, D, true, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1,
@@ -1107,6 +1122,7 @@ plora_status attend(const void* q, int64_t q_token, int64_t q_head, const plora_
   a.tile = reinterpret_cast<const Item*>(p + l.tile);
   a.order = reinterpret_cast<const int32_t*>(p + l.order);
   a.info = reinterpret_cast<const ReqInfo*>(p + l.req);
+  a.tile_cap = b.tile_cap;
   a.batch = s.batch;
   a.T = s.T;
   a.r = b.r;
