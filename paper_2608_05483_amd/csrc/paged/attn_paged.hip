@@ -870,9 +870,9 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
 // x 64 heads, 59 pieces: 10.0 us with a wavefront a row, about 5 so).  Rows that the
 // items wrote themselves are left, rows without a key get zeros.  Bound by reading
 // the partials, or by the latency of its chain of loads.
-template <class Ty, int D, bool WIDE>
+template <class Ty, int D, bool WIDE, int kAt>
 __device__ __forceinline__ void merge_token(const AttnArgs& a, int t, int32_t per) {
-  constexpr int kL = D / 4, kRows = 64 / kL, kAt = 8;
+  constexpr int kL = D / 4, kRows = 64 / kL;
   __shared__ f32x4 s_o[WIDE ? kWaves : 1][64];
   __shared__ float s_m[WIDE ? kWaves : 1][kRows], s_l[WIDE ? kWaves : 1][kRows];
   const int lane = threadIdx.x & 63, wv = uniform(threadIdx.x >> 6);
@@ -980,15 +980,20 @@ __device__ __forceinline__ void merge_token(const AttnArgs& a, int t, int32_t pe
   }
 }
 
+// kAt: partials of a row on their way together.  Many rows hide the latency among
+// themselves, so four, for which twice the wavefronts fit, are faster there (69 000 rows
+// of 3 pieces 32 us with eight, 21 with four; 33 000 of 2 13.4 and 11.4); few rows, which
+// have more pieces, take eight (1536 rows of 42 pieces 7.5 us, 9.0 with four).
+constexpr int64_t kManyRows = 16384;
 // Many tokens are kMergeTokens work groups' in turn, which look at 64 of theirs at
 // once, a lane each, for those that have something to merge: few do among the tokens
 // of long prompts, and those of one request lie with different work groups (16247
 // tokens, none of them: 10.3 us with a work group each, 4.8 so).
 constexpr int kMergeTokens = 2048;
-template <class Ty, int D, bool WIDE>
-__global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
+template <class Ty, int D, bool WIDE, int kAt>
+__global__ __launch_bounds__(kNT, kAt == 8 ? 4 : 8) void merge_kernel(AttnArgs a, int32_t per) {
   const int n = gridDim.x, lane = threadIdx.x & 63;
-  if (n >= a.T) return merge_token<Ty, D, WIDE>(a, blockIdx.x, per);
+  if (n >= a.T) return merge_token<Ty, D, WIDE, kAt>(a, blockIdx.x, per);
   for (int t0 = blockIdx.x; t0 < a.T; t0 += 64 * n) {
     const int t = t0 + lane * n;
     bool any = false;
@@ -1000,7 +1005,7 @@ __global__ __launch_bounds__(kNT) void merge_kernel(AttnArgs a, int32_t per) {
     while (mask) {
       const int i = __builtin_ctzll(mask);
       mask &= mask - 1;
-      merge_token<Ty, D, WIDE>(a, t0 + i * n, per);
+      merge_token<Ty, D, WIDE, kAt>(a, t0 + i * n, per);
     }
   }
 }
@@ -1038,13 +1043,15 @@ plora_status launch(const AttnArgs& a, const Bounds& b, hipStream_t stream) {
   // token per work group: all, or one pass where the tokens are few.
   const int heads = a.kv_heads * a.r, rows = 256 / D;
   if ((int64_t)a.T * heads <= 1024) {
-    hipLaunchKernelGGL((merge_kernel<Ty, D, true>), dim3(a.T, (heads + rows - 1) / rows),
+    hipLaunchKernelGGL((merge_kernel<Ty, D, true, 8>), dim3(a.T, (heads + rows - 1) / rows),
                        dim3(kNT), 0, stream, a, rows);
   } else {
     const int per = a.T < kMergeTokens ? kWaves * rows : heads;
-    hipLaunchKernelGGL((merge_kernel<Ty, D, false>),
-                       dim3(std::min(a.T, kMergeTokens), (heads + per - 1) / per), dim3(kNT), 0,
-                       stream, a, per);
+    const dim3 grid(std::min(a.T, kMergeTokens), (heads + per - 1) / per);
+    if ((int64_t)a.T * heads <= kManyRows)
+      hipLaunchKernelGGL((merge_kernel<Ty, D, false, 8>), grid, dim3(kNT), 0, stream, a, per);
+    else
+      hipLaunchKernelGGL((merge_kernel<Ty, D, false, 4>), grid, dim3(kNT), 0, stream, a, per);
   }
   return launch_status();
 }
