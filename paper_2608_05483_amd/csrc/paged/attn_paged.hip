@@ -691,7 +691,11 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
               s[b][i] = 32 * b + 8 * (i >> 2) + (i & 3) < lim ? s[b][i] : -INFINITY;
           if constexpr (TREE) any = any || lim > 0;
         } else {
-          const int cached = fresh.past - k0 - 4 * h;
+          // (four keys at a time, and the comparisons with the limit made here: else the
+          // masks of all keys are held in scalar registers, and what the loop needs there
+          // is moved away and back in every step)
+          int cached = fresh.past - k0 - 4 * h, own = lim;
+          asm volatile("" : "+v"(cached), "+v"(own));
           const i32x4* np = reinterpret_cast<const i32x4*>(sn) + h;
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
@@ -699,12 +703,13 @@ __device__ __forceinline__ void tile_item(const AttnArgs& a, const Item& it, int
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
               const int at = 8 * j + e;
-              const bool seen = (at < lim) & ((at < cached) | ((first[e] <= x.number) &
+              const bool seen = (at < own) & ((at < cached) | ((first[e] <= x.number) &
                                                                (x.number <= last[e])));
               const int i = 4 * (j & 3) + e;
               s[j >> 2][i] = seen ? s[j >> 2][i] : -INFINITY;
               any |= seen;
             }
+            __builtin_amdgcn_sched_barrier(0);
           }
         }
       }
