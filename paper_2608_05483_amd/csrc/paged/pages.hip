@@ -312,9 +312,11 @@ struct MoveArgs {
 };
 
 // A work group copies a page's keys in k or v of a layer: neighbouring threads take
-// neighbouring units of a row, kAtOnce rows of a thread on their way together.  Bound by
-// reading and writing.
-constexpr int kAtOnce = 8;
+// neighbouring units of a row, kCopyAtOnce rows of a thread on their way together, written
+// non-temporally (nobody reads them soon).  Bound by reading and writing: 297 MB, read
+// and written, in 49 us (6.0 TB/s); with plain stores 55, and with 8 rows 63 (non-temporal
+// 51); loads non-temporal as well 73.
+constexpr int kCopyAtOnce = 16;
 template <class U>
 __global__ __launch_bounds__(kNT) void copy_kernel(MoveArgs a, const int32_t* copies, int32_t cap,
                                                    const int32_t* n_copies) {
@@ -330,18 +332,19 @@ __global__ __launch_bounds__(kNT) void copy_kernel(MoveArgs a, const int32_t* co
   const int rows = keys * a.kv_heads;
   if ((int)threadIdx.x >= wide * per) return;
   for (int u = threadIdx.x % wide; u < a.units; u += wide) {
-    for (int r0 = threadIdx.x / wide; r0 < rows; r0 += per * kAtOnce) {
-      U v[kAtOnce];
-      int64_t off[kAtOnce];
+    for (int r0 = threadIdx.x / wide; r0 < rows; r0 += per * kCopyAtOnce) {
+      U v[kCopyAtOnce];
+      int64_t off[kCopyAtOnce];
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i) {
+      for (int i = 0; i < kCopyAtOnce; ++i) {
         const int r = min(r0 + i * per, rows - 1), h = (uint32_t)r / (uint32_t)keys;
         off[i] = h * a.head_stride + (r - h * keys) * a.token_stride + (int64_t)u * sizeof(U);
         v[i] = *reinterpret_cast<const U*>(x + off[i]);
       }
 #pragma unroll
-      for (int i = 0; i < kAtOnce; ++i)
-        if (r0 + i * per < rows) *reinterpret_cast<U*>(y + off[i]) = v[i];
+      for (int i = 0; i < kCopyAtOnce; ++i)
+        if (r0 + i * per < rows)
+          __builtin_nontemporal_store(v[i], reinterpret_cast<U*>(y + off[i]));
     }
   }
 }
@@ -350,7 +353,9 @@ __global__ __launch_bounds__(kNT) void copy_kernel(MoveArgs a, const int32_t* co
 // request's path, which nobody else touches.  A lane looks up a move, 64 at once.  Up to
 // kAtOnce keys are read before they are stored where that is the same as one after the
 // other: a path's numbers are not below their places, so no key of the ones read
-// together is where an earlier one of them goes.  Bound by latency.
+// together is where an earlier one of them goes.  Bound by latency (64 paths of up to 9
+// keys in 16 layers 6.7 us, 7.4 with plain stores).
+constexpr int kAtOnce = 8;
 template <class U>
 __global__ __launch_bounds__(kNT) void compact_kernel(MoveArgs a, const int32_t* q_start,
                                                       const int32_t* req, const int64_t* slot,
@@ -406,7 +411,7 @@ __global__ __launch_bounds__(kNT) void compact_kernel(MoveArgs a, const int32_t*
       }
 #pragma unroll
       for (int q = 0; q < kAtOnce; ++q)
-        if (q < k && mine) *reinterpret_cast<U*>(pool + y[q]) = v[q];
+        if (q < k && mine) __builtin_nontemporal_store(v[q], reinterpret_cast<U*>(pool + y[q]));
     }
   }
 }
