@@ -99,6 +99,9 @@ class Remap:
         self.struct = plora_kv_batch(new_batch, max_pages, self.table.data_ptr(),
                                      self.kv_len.data_ptr())
         self.ref = ctypes.byref(self.struct)
+        self.out = (self.copies.data_ptr(), self.meta.data_ptr(), self.ws.data_ptr(),
+                    self.ws.numel())
+        self.listed = (self.copies.data_ptr(), new_batch, self.meta.data_ptr() + 4)
 
 
 class Caches:
@@ -130,15 +133,16 @@ def kv_remap(table, kv_len, src, keep, pool: PagePool, free_head, free_next, rem
     dev, n = remap.dev, remap.old_batch
     if table.dim() != 2 or table.shape[0] < n:
         raise ValueError("table: [old_batch, max_pages] expected")
-    _on("pool", pool.shares, dev)
+    if pool.dev != dev:
+        _on("pool", pool.shares, dev)
     old = plora_kv_batch(n, table.shape[1], _ints("table", table, _I32, 0, dev),
                          _ints("kv_len", kv_len, _I32, n, dev))
     _ok("plora_kv_remap", lib.plora_kv_remap(
         ctypes.byref(old), _ints("src", src, _I32, remap.batch, dev),
         None if keep is None else _ints("keep", keep, _I32, remap.batch, dev), remap.page_size,
         pool.ref, _ints("free_head", free_head, _I32, 1, dev),
-        _ints("free_next", free_next, _I32, 1, dev), remap.ref, remap.copies.data_ptr(),
-        remap.meta.data_ptr(), remap.ws.data_ptr(), remap.ws.numel(), _stream(stream, dev)))
+        _ints("free_next", free_next, _I32, 1, dev), remap.ref, *remap.out,
+        _stream(stream, dev)))
 
 
 def kv_copy(caches: Caches, remap: Remap, stream=None) -> None:
@@ -146,11 +150,11 @@ def kv_copy(caches: Caches, remap: Remap, stream=None) -> None:
     if caches.n == 0:
         return
     dev = caches.dev
-    _on("remap", remap.meta, dev)
+    if remap.dev != dev:
+        _on("remap", remap.meta, dev)
     if remap.page_size != caches.page_size:
         raise ValueError("remap: pages of another size than the caches'")
-    _ok("plora_kv_copy", lib.plora_kv_copy(caches.array, caches.n, remap.copies.data_ptr(),
-                                           remap.batch, remap.meta.data_ptr() + 4,
+    _ok("plora_kv_copy", lib.plora_kv_copy(caches.array, caches.n, *remap.listed,
                                            _stream(stream, dev)))
 
 

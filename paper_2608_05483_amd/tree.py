@@ -75,12 +75,15 @@ class Accepted:
         self.token = torch.full((step.batch,), -1, dtype=dtype, device=device)
         self.kv_len = torch.zeros(step.batch, **i32)
         self.dev = self.path.get_device()
+        self.out = (self.path.data_ptr(), self.count.data_ptr(), self.token.data_ptr(),
+                    self.kv_len.data_ptr())
 
 
 def tree_plan(parent, step: Step, tree: Tree, stream=None) -> None:
     """parent int32 [T]: a node's parent by its number in its request, -1 for a root."""
     dev = step.dev
-    _on("tree", tree.pos, dev)
+    if tree.dev != dev:
+        _on("tree", tree.pos, dev)
     _ok("plora_tree_plan", lib.plora_tree_plan(
         _ints("parent", parent, _I32, step.T, dev), step.ref, tree.ref, _stream(stream, dev)))
 
@@ -106,15 +109,15 @@ def tree_accept(parent, drafted, target, step: Step, accepted: Accepted, given=N
     """drafted, target [T], of accepted's type; given int32 [batch]: how many of a
     request's first nodes are certain (None: the first)."""
     dev, dt, T = step.dev, accepted.dtype, step.T
-    _on("accepted", accepted.path, dev)
+    if accepted.dev != dev:
+        _on("accepted", accepted.path, dev)
     if accepted.T != T or accepted.batch != step.batch:
         raise ValueError("accepted: made for another step")
     _ok("plora_tree_accept", lib.plora_tree_accept(
         _ints("parent", parent, _I32, T, dev), _ints("drafted", drafted, dt, T, dev),
         _ints("target", target, dt, T, dev), 4 if dt is _I32 else 8,
         None if given is None else _ints("given", given, _I32, step.batch, dev), step.ref,
-        accepted.path.data_ptr(), accepted.count.data_ptr(), accepted.token.data_ptr(),
-        accepted.kv_len.data_ptr(), _stream(stream, dev)))
+        *accepted.out, _stream(stream, dev)))
 
 
 def run_layers(step: Step, plan: AttnPlan, tree: Tree, layers, turns, scale: float,
