@@ -149,7 +149,8 @@ __constant__ const int kTry[kTries] = {256, 320, 384, 448, 512, 640, 768, 1024};
 static_assert(kTileTarget == 1024, "the finest cut tried bounds the items");
 constexpr int kOwn = 8;
 // Tile items are listed by the length of their keys, in quarters of the longest's, the
-// longest first: a long one that is begun last is waited for.
+// longest first: a long one that is begun last is waited for.  (Where one round takes
+// all, their order is none.)
 constexpr int kClasses = 4;
 __device__ __forceinline__ int class_of(int keys, int longest) {
   const int64_t k = 4 * (int64_t)keys;
@@ -174,7 +175,7 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
   __shared__ uint32_t red_class[kWaves][kClasses];
   __shared__ double s_work[kWaves][2];
   __shared__ int64_t s_cost[kTries];
-  __shared__ int s_per[kTries], s_long[kTries];
+  __shared__ int s_per[kTries], s_long[kTries];  // (longest piece; 0: one round takes all)
   const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   Kept y;
   {
@@ -319,16 +320,16 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
     if (lane == 63) {
       s_cost[wv] = (items * a.kv_heads + kTileSlots - 1) / kTileSlots * (longest + kTileStart);
       s_per[wv] = per;
-      s_long[wv] = longest;
+      s_long[wv] = items * a.kv_heads > kTileSlots ? longest : 0;
     }
     __syncthreads();
     int64_t least = INT64_MAX;
 #pragma unroll
     for (int k = 0; k < kTries; ++k)
       if (s_cost[k] < least) least = s_cost[k], tile_keys = s_per[k], longest_tile = s_long[k];
-    // where each class begins
+    // where each class begins (of one round all are of the first)
     uint32_t n[kClasses] = {};
-    for (int i = tid; i < n_sets; i += kNT) {
+    for (int i = tid; longest_tile > 0 && i < n_sets; i += kNT) {
       int rows, keys;
       set_of(i, rows, keys);
       if (rows <= kFew) continue;
@@ -338,13 +339,14 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
 #pragma unroll
       for (int j = 0; j < kClasses; ++j) n[j] = k == j ? AddCount{}(n[j], z) : n[j];
     }
-    uint32_t all[kClasses] = {};
-    scan(n, all, red_class);
-    uint32_t at = 0;
+    if (longest_tile > 0) {
+      uint32_t all[kClasses] = {}, at = 0;
+      scan(n, all, red_class);
 #pragma unroll
-    for (int j = 0; j < kClasses; ++j) {
-      sum[3 + j] = at;
-      at = AddCount{}(at, all[j]);
+      for (int j = 0; j < kClasses; ++j) {
+        sum[3 + j] = at;
+        at = AddCount{}(at, all[j]);
+      }
     }
   }
   // items
@@ -444,7 +446,7 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
     h.left = s_left;
     h.few = min((int)sum[0], a.few_cap);
     h.later = min((int)sum[2], a.few_cap - h.few);
-    h.tiles = min((int)sum[2 + kClasses], a.tile_cap);
+    h.tiles = min((int)sum[longest_tile > 0 ? 2 + kClasses : 3], a.tile_cap);
     h.part_rows = min((int)sum[1], a.part_cap);
     h.few_keys = few_keys;
     h.tile_keys = tile_keys;
