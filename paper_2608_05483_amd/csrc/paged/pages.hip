@@ -526,6 +526,12 @@ extern "C" plora_status plora_kv_remap(const plora_kv_batch* old_batch, const in
       (n.batch > 0 && (!n.kv_len || !src || !copies)) ||
       (n.batch > 0 && n.max_pages > 0 && !n.table))
     return PLORA_ERR_INVALID_ARG;
+  if ((o.batch > 0 && n.batch > 0 && (o.kv_len == n.kv_len || (o.table && o.table == n.table))) ||
+      free_head == free_next || (n.batch > 0 && (src == n.kv_len || keep == n.kv_len)))
+    return PLORA_ERR_INVALID_ARG;
+  // (entries of a chunk of requests are counted in 32 bits)
+  if ((int64_t)std::min(o.batch, kFT) * o.max_pages > INT32_MAX - kTurn)
+    return PLORA_ERR_UNSUPPORTED;
   if (!aligned(ws, 16) || !aligned(pool->scratch, 8)) return PLORA_ERR_UNSUPPORTED;
   const RemapWs w = remap_ws(o.batch, n.batch);
   if (ws_bytes < w.bytes) return PLORA_ERR_WORKSPACE_TOO_SMALL;
@@ -603,6 +609,8 @@ extern "C" plora_status plora_kv_compact(const plora_kv_cache* caches, int32_t l
     return PLORA_ERR_INVALID_ARG;
   const int columns = a.kv_heads * a.units, threads = std::min(kNT, (columns + 63) / 64 * 64);
   const int parts = (columns + threads - 1) / threads;
+  if ((int64_t)step->batch * parts * threads > (int64_t)UINT32_MAX)   // threads of a launch
+    return PLORA_ERR_UNSUPPORTED;
   return by_layers(caches, layers, a, bytes, [&](auto u, int n) {
     hipLaunchKernelGGL(compact_kernel<decltype(u)>, dim3(step->batch * parts, n, 2), dim3(threads),
                        0, stream, a, step->q_start, step->req, step->slot, path, count, step->T,

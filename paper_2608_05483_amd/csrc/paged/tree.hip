@@ -275,6 +275,7 @@ extern "C" plora_status plora_tree_accept(const int32_t* parent, const void* dra
   if ((step->T > 0 && (!parent || !drafted || !target || !path)) ||
       (step->batch > 0 && (!count || !token || !kv_len)))
     return PLORA_ERR_INVALID_ARG;
+  if (step->batch > 0 && kv_len == step->kv_len) return PLORA_ERR_INVALID_ARG;
   if (!aligned(drafted, token_bytes) || !aligned(target, token_bytes) ||
       !aligned(token, token_bytes))
     return PLORA_ERR_UNSUPPORTED;

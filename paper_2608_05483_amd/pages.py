@@ -13,9 +13,10 @@ import ctypes
 
 import torch
 
-from .paged import META_WORDS, _I32, KVCache, Step, _ints, _on, _ok, _stream, plora_kv_cache, \
+from .paged import META_WORDS, _I32, KVCache, Step, _ints, _on, _stream, plora_kv_cache, \
     plora_kv_step
 from .plora import lib
+from .tree import _launch
 
 MAX_LAYERS = 1024
 
@@ -137,12 +138,12 @@ def kv_remap(table, kv_len, src, keep, pool: PagePool, free_head, free_next, rem
         _on("pool", pool.shares, dev)
     old = plora_kv_batch(n, table.shape[1], _ints("table", table, _I32, 0, dev),
                          _ints("kv_len", kv_len, _I32, n, dev))
-    _ok("plora_kv_remap", lib.plora_kv_remap(
-        ctypes.byref(old), _ints("src", src, _I32, remap.batch, dev),
-        None if keep is None else _ints("keep", keep, _I32, remap.batch, dev), remap.page_size,
-        pool.ref, _ints("free_head", free_head, _I32, 1, dev),
-        _ints("free_next", free_next, _I32, 1, dev), remap.ref, *remap.out,
-        _stream(stream, dev)))
+    _launch("plora_kv_remap", lib.plora_kv_remap, dev, ctypes.byref(old),
+            _ints("src", src, _I32, remap.batch, dev),
+            None if keep is None else _ints("keep", keep, _I32, remap.batch, dev),
+            remap.page_size, pool.ref, _ints("free_head", free_head, _I32, 1, dev),
+            _ints("free_next", free_next, _I32, 1, dev), remap.ref, *remap.out,
+            _stream(stream, dev))
 
 
 def kv_copy(caches: Caches, remap: Remap, stream=None) -> None:
@@ -154,8 +155,8 @@ def kv_copy(caches: Caches, remap: Remap, stream=None) -> None:
         _on("remap", remap.meta, dev)
     if remap.page_size != caches.page_size:
         raise ValueError("remap: pages of another size than the caches'")
-    _ok("plora_kv_copy", lib.plora_kv_copy(caches.array, caches.n, *remap.listed,
-                                           _stream(stream, dev)))
+    _launch("plora_kv_copy", lib.plora_kv_copy, dev, caches.array, caches.n, *remap.listed,
+            _stream(stream, dev))
 
 
 def kv_compact(caches: Caches, step: Step, path, count, stream=None) -> None:
@@ -165,6 +166,6 @@ def kv_compact(caches: Caches, step: Step, path, count, stream=None) -> None:
     dev = caches.dev
     if step.dev != dev:
         raise ValueError("step: on another device than the caches")
-    _ok("plora_kv_compact", lib.plora_kv_compact(
-        caches.array, caches.n, step.ref, _ints("path", path, _I32, step.T, dev),
-        _ints("count", count, _I32, step.batch, dev), _stream(stream, dev)))
+    _launch("plora_kv_compact", lib.plora_kv_compact, dev, caches.array, caches.n, step.ref,
+            _ints("path", path, _I32, step.T, dev),
+            _ints("count", count, _I32, step.batch, dev), _stream(stream, dev))

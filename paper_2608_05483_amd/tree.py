@@ -44,6 +44,15 @@ def _declare(L) -> None:
 _declare(lib)
 
 
+def _launch(name: str, fn, dev: int, *args) -> None:
+    """The call with GPU dev, which its tensors are on, as the current one: a launch on
+    the default stream goes to the current GPU."""
+    if torch.cuda.current_device() != dev:
+        with torch.cuda.device(dev):
+            return _ok(name, fn(*args))
+    _ok(name, fn(*args))
+
+
 class Tree:
     """What a step knows of its trees (plora_tree): pos int32 [T] for the rotation,
     span int32 [T, 2], info int32 [batch, 2] (1 for a tree that is no chain; its cut
@@ -84,8 +93,8 @@ def tree_plan(parent, step: Step, tree: Tree, stream=None) -> None:
     dev = step.dev
     if tree.dev != dev:
         _on("tree", tree.pos, dev)
-    _ok("plora_tree_plan", lib.plora_tree_plan(
-        _ints("parent", parent, _I32, step.T, dev), step.ref, tree.ref, _stream(stream, dev)))
+    _launch("plora_tree_plan", lib.plora_tree_plan, dev,
+            _ints("parent", parent, _I32, step.T, dev), step.ref, tree.ref, _stream(stream, dev))
 
 
 def attn_tree(q, cache: KVCache, step: Step, plan: AttnPlan, tree: Tree, scale: float, out,
@@ -98,10 +107,9 @@ def attn_tree(q, cache: KVCache, step: Step, plan: AttnPlan, tree: Tree, scale: 
         raise ValueError("q, out: the plan's [T, heads, head_dim] expected")
     if step.dev != dev or plan.dev != dev or tree.dev != dev:
         raise ValueError("step, plan, tree: on another device than the cache")
-    _ok("plora_attn_tree", lib.plora_attn_tree(
-        pq, qt, qh, cache.ref, step.ref, plan.ref, tree.ref, scale, plan.plan.data_ptr(),
-        plan.plan.numel(), po, ot, oh, plan.ws.data_ptr(), plan.ws.numel(),
-        _stream(stream, dev)))
+    _launch("plora_attn_tree", lib.plora_attn_tree, dev, pq, qt, qh, cache.ref, step.ref, plan.ref,
+            tree.ref, scale, plan.plan.data_ptr(), plan.plan.numel(), po, ot, oh,
+            plan.ws.data_ptr(), plan.ws.numel(), _stream(stream, dev))
 
 
 def tree_accept(parent, drafted, target, step: Step, accepted: Accepted, given=None,
@@ -113,11 +121,11 @@ def tree_accept(parent, drafted, target, step: Step, accepted: Accepted, given=N
         _on("accepted", accepted.path, dev)
     if accepted.T != T or accepted.batch != step.batch:
         raise ValueError("accepted: made for another step")
-    _ok("plora_tree_accept", lib.plora_tree_accept(
-        _ints("parent", parent, _I32, T, dev), _ints("drafted", drafted, dt, T, dev),
-        _ints("target", target, dt, T, dev), 4 if dt is _I32 else 8,
-        None if given is None else _ints("given", given, _I32, step.batch, dev), step.ref,
-        *accepted.out, _stream(stream, dev)))
+    _launch("plora_tree_accept", lib.plora_tree_accept, dev,
+            _ints("parent", parent, _I32, T, dev), _ints("drafted", drafted, dt, T, dev),
+            _ints("target", target, dt, T, dev), 4 if dt is _I32 else 8,
+            None if given is None else _ints("given", given, _I32, step.batch, dev), step.ref,
+            *accepted.out, _stream(stream, dev))
 
 
 def run_layers(step: Step, plan: AttnPlan, tree: Tree, layers, turns, scale: float,

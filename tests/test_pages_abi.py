@@ -40,26 +40,33 @@ def batch(**kw):
     return K.plora_kv_batch(**b)
 
 
-def remap_status(o=None, n=None, p=None, src=FAKE, keep=None, page=16, head=FAKE, nxt=FAKE,
+def new(**kw):
+    return batch(**dict(dict(table=FAKE + 4096, kv_len=FAKE + 4096), **kw))
+
+
+def remap_status(o=None, n=None, p=None, src=FAKE, keep=None, page=16, head=FAKE, nxt=FAKE + 64,
                  copies=FAKE, meta=FAKE, ws=FAKE, wb=None):
-    o, n, p = o or batch(), n or batch(), p or pool()
+    o, n, p = o or batch(), n or new(), p or pool()
     wb = K.kv_remap_workspace_bytes(3, 3) if wb is None else wb
     return P.lib.plora_kv_remap(ctypes.byref(o), src, keep, page, ctypes.byref(p), head, nxt,
                                 ctypes.byref(n), copies, meta, ws, wb, None)
 
 
 @pytest.mark.parametrize("kw,want", [
-    (dict(o=batch(batch=-1)), INV), (dict(n=batch(batch=-1)), INV),
-    (dict(o=batch(max_pages=-1)), INV), (dict(n=batch(max_pages=-1)), INV),
+    (dict(o=batch(batch=-1)), INV), (dict(n=new(batch=-1)), INV),
+    (dict(o=batch(max_pages=-1)), INV), (dict(n=new(max_pages=-1)), INV),
     (dict(p=pool(n_pages=-1)), INV), (dict(p=pool(n_free=-1)), INV),
     (dict(p=pool(shares=None)), INV), (dict(p=pool(free_pages=None)), INV),
     (dict(p=pool(scratch=None)), INV), (dict(src=None), INV), (dict(head=None), INV),
     (dict(nxt=None), INV), (dict(copies=None), INV), (dict(meta=None), INV), (dict(ws=None), INV),
     (dict(o=batch(table=None)), INV), (dict(o=batch(kv_len=None)), INV),
-    (dict(n=batch(table=None)), INV), (dict(n=batch(kv_len=None)), INV),
+    (dict(n=new(table=None)), INV), (dict(n=new(kv_len=None)), INV),
+    (dict(n=new(table=FAKE)), INV), (dict(n=new(kv_len=FAKE)), INV), (dict(nxt=FAKE), INV),
+    (dict(src=FAKE + 4096), INV), (dict(keep=FAKE + 4096), INV),
+    (dict(o=batch(batch=64, max_pages=1 << 25)), UNS),
     (dict(page=24), UNS), (dict(page=8), UNS), (dict(page=512), UNS),
-    (dict(o=batch(batch=G.MAX_BATCH + 1)), UNS), (dict(n=batch(batch=G.MAX_BATCH + 1)), UNS),
-    (dict(o=batch(max_pages=(1 << 26) + 1)), UNS), (dict(n=batch(max_pages=(1 << 26) + 1)), UNS),
+    (dict(o=batch(batch=G.MAX_BATCH + 1)), UNS), (dict(n=new(batch=G.MAX_BATCH + 1)), UNS),
+    (dict(o=batch(max_pages=(1 << 26) + 1)), UNS), (dict(n=new(max_pages=(1 << 26) + 1)), UNS),
     (dict(ws=FAKE + 8), UNS), (dict(p=pool(scratch=FAKE + 4)), UNS), (dict(wb=16), SMALL),
 ])
 def test_remap_refusals(kw, want):
@@ -112,6 +119,8 @@ def test_copy_refusals(kw, want):
     (dict(s=step(req=None)), INV), (dict(s=step(slot=None)), INV), (dict(s=step(batch=-1)), INV),
     (dict(s=step(T=-1)), INV), (dict(s=step(page_size=32)), INV),
     (dict(s=step(batch=G.MAX_BATCH + 1)), UNS), (dict(s=step(T=G.MAX_TOKENS + 1)), UNS),
+    (dict(cs=array(cache(kv_heads=1024, head_dim=511)), layers=1,
+          s=step(batch=G.MAX_BATCH)), UNS),
     (dict(s=step(batch=0), path=None), OK), (dict(s=step(T=0), path=None), OK),
     (dict(layers=0), OK),
 ])

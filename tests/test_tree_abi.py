@@ -84,7 +84,7 @@ def test_attn_tree_refusals(kw, want):
 
 
 def accept_status(s=None, parent=FAKE, drafted=FAKE, target=FAKE, nb=4, given=FAKE, path=FAKE,
-                  count=FAKE, token=FAKE, kv=FAKE):
+                  count=FAKE, token=FAKE, kv=FAKE + 4096):
     s = s or step()
     return P.lib.plora_tree_accept(parent, drafted, target, nb, given, ctypes.byref(s), path, count,
                                    token, kv, None)
@@ -95,7 +95,7 @@ def accept_status(s=None, parent=FAKE, drafted=FAKE, target=FAKE, nb=4, given=FA
     (dict(path=None), INV), (dict(count=None), INV), (dict(token=None), INV), (dict(kv=None), INV),
     (dict(s=step(q_start=None)), INV), (dict(s=step(kv_len=None)), INV),
     (dict(s=step(req=None)), INV), (dict(s=step(batch=-1)), INV), (dict(s=step(T=-1)), INV),
-    (dict(nb=2), UNS), (dict(nb=0), UNS), (dict(nb=8, drafted=FAKE + 4), UNS),
+    (dict(kv=FAKE), INV), (dict(nb=2), UNS), (dict(nb=0), UNS), (dict(nb=8, drafted=FAKE + 4), UNS),
     (dict(nb=8, target=FAKE + 4), UNS), (dict(nb=8, token=FAKE + 4), UNS),
     (dict(s=step(batch=G.MAX_BATCH + 1)), UNS), (dict(s=step(T=G.MAX_TOKENS + 1)), UNS),
     (dict(s=step(batch=0, T=0), parent=None), OK),
@@ -126,6 +126,30 @@ def test_binding_refuses_what_pointers_cannot_tell():
         R.tree_accept(i(6), i(6), i(6), other, a)
     with pytest.raises(ValueError):              # all on the host
         R.tree_plan(i(5), s, t)
+
+
+def test_calls_are_made_with_the_tensors_gpu_current(monkeypatch):
+    import torch
+    now, seen = [0], []
+
+    class Device:
+        def __init__(self, d):
+            self.d = d
+
+        def __enter__(self):
+            self.was, now[0] = now[0], self.d
+
+        def __exit__(self, *a):
+            now[0] = self.was
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    for dev in (0, 3):
+        R._launch("call", lambda *a: seen.append((now[0], a)) or OK, dev, 1, 2)
+        with pytest.raises(P.PloraError):
+            R._launch("call", lambda: INV, dev)
+        assert now == [0]
+    assert seen == [(0, (1, 2)), (3, (1, 2))]
 
 
 # ---- the oracle's pins ------------------------------------------------------------------
