@@ -38,12 +38,12 @@ struct TreeArgs {
   int2* info;
 };
 
-// A work group a request.  With the parents in LDS a node walks to its root three
-// times: for its depth, to add itself to the size of each of its ancestors, and to add
-// up the preorder number: one for each ancestor, and the sizes of the earlier siblings
-// of each node on the path.  Those are found by looking at all nodes, four at a time,
+// A work group a request.  With the parents in LDS a node walks to its root twice: to
+// add itself to the size of each of its ancestors, and to add up its depth and its
+// preorder number: one for each ancestor, and the sizes of the earlier siblings of each
+// node on the path.  Those are found by looking at all nodes, four at a time,
 // the same ones in all lanes, so that many reads are on their way (24 requests of 100
-// to 250 nodes: 11.6 us, 19 with each lane going from its parent on).  Whole numbers, so
+// to 250 nodes: 11.3 us, 19 with each lane going from its parent on).  Whole numbers, so
 // the order of the additions changes nothing.  Bound by latency: 64 requests of 20 to 60
 // nodes 6 us, as long as plora_kv_plan for the same step.
 __global__ __launch_bounds__(kNT) void tree_plan_kernel(TreeArgs a) {
@@ -76,15 +76,21 @@ __global__ __launch_bounds__(kNT) void tree_plan_kernel(TreeArgs a) {
   }
   int cut = 0;
   for (int i = tid; i < x.n; i += kNT) {
-    int p = i, q = s_par[i];
-    while (q >= 0 && q < p) p = q, q = s_par[p];
-    if (q != -1) {
-      s_sib[i] = -1;
-      ++cut;
-      continue;
+    int p = i, q;
+    while (true) {
+      atomicAdd(&s_size[p], 1);
+      q = s_par[p];
+      if (q < 0 || q >= p) break;
+      p = q;
     }
-    s_sib[i] = 0;
-    for (p = i; p >= 0; p = s_par[p]) atomicAdd(&s_size[p], 1);
+    s_sib[i] = q == -1 ? 0 : -1;
+    if (q != -1) {                       // no root is reached: taken back
+      ++cut;
+      for (q = i;; q = s_par[q]) {
+        atomicAdd(&s_size[q], -1);
+        if (q == p) break;
+      }
+    }
   }
   if (cut) atomicAdd(&s_cut, cut);
   __syncthreads();

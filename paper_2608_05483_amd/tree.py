@@ -43,11 +43,13 @@ def _declare(L) -> None:
 
 _declare(lib)
 
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
 
 def _launch(name: str, fn, dev: int, *args) -> None:
     """The call with GPU dev, which its tensors are on, as the current one: a launch on
     the default stream goes to the current GPU."""
-    if torch.cuda.current_device() != dev:
+    if _device() != dev:
         with torch.cuda.device(dev):
             return _ok(name, fn(*args))
     _ok(name, fn(*args))

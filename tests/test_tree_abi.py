@@ -142,7 +142,7 @@ def test_calls_are_made_with_the_tensors_gpu_current(monkeypatch):
         def __exit__(self, *a):
             now[0] = self.was
 
-    monkeypatch.setattr(torch.cuda, "current_device", lambda: now[0])
+    monkeypatch.setattr(R, "_device", lambda: now[0])
     monkeypatch.setattr(torch.cuda, "device", Device)
     for dev in (0, 3):
         R._launch("call", lambda *a: seen.append((now[0], a)) or OK, dev, 1, 2)
