@@ -271,6 +271,27 @@ def test_compact(G, K, dt, form, D, layers, KH):
         assert np.array_equal(w.double().cpu().numpy(), y)
 
 
+@pytest.mark.parametrize("down", [1, 3, 64, 100])
+def test_compact_of_long_paths(G, K, down):
+    """More moves than are looked up at once, each onto a place that another is read
+    from later."""
+    rng = np.random.default_rng(down)
+    cs, xs, ws = caches(G, K, 2, 40, 3, 16, 64, BF, "plain")
+    new = [210, 66]
+    step = stepped(G, [7, 30], new, 16, 40, rng)
+    path, count = np.full(sum(new) + 2, -1), []
+    for b, n in enumerate(new):
+        lo, a = sum(new[:b]), max(n - down, 0)
+        path[lo:lo + a] = np.arange(a) + down
+        count.append(a)
+    want = [w.double().cpu().numpy() for w in ws]
+    K.kv_compact(cs, step, i32(path), i32(count))
+    s = {k: arr(getattr(step, k)) for k in ("q_start", "req", "slot")}
+    for w, y in zip(ws, want):
+        OG.compact(y, s["q_start"], s["req"], s["slot"], path, count)
+        assert np.array_equal(w.double().cpu().numpy(), y)
+
+
 def test_compact_with_slots_outside_the_pool(G, K):
     rng = np.random.default_rng(0)
     cs, xs, ws = caches(G, K, 2, 8, 2, 16, 64, BF, "plain")
