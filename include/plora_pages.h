@@ -83,7 +83,7 @@ typedef struct {
  * that it holds.  The two batches' arrays, src, keep, free_head, free_next, copies and
  * meta must not overlap.  The old batch's rows, of 1024 requests, have up to 2^31 - 2^14
  * entries.  ws: plora_kv_remap_workspace_bytes, 16-byte aligned, no contents needed.
- * One launch for small batches, else two.
+ * One launch for small batches, two or three for larger ones.
  */
 size_t plora_kv_remap_workspace_bytes(int32_t old_batch, int32_t new_batch);
 plora_status plora_kv_remap(const plora_kv_batch* old_batch, const int32_t* src,

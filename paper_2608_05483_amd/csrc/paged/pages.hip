@@ -109,6 +109,34 @@ __global__ __launch_bounds__(kNT) void remap_rows_kernel(RemapArgs a) {
   remap_row<kNT>(a, blockIdx.x, red);
 }
 
+// A dropped page that nobody holds carries the number of the lowest request that dropped
+// it, as a mark below all counts.
+constexpr int kMark = INT32_MIN / 2;     // (the number is added)
+
+// An old request's dropped entries by a work group: the marks, and what of the entries
+// has to be looked at again, from the first page without a holder to the last.  Of a page
+// that others go on with there is no more to do: where forks of long contexts end
+// together, of each only its last page or two.
+__global__ __launch_bounds__(kNT) void remap_mark_kernel(RemapArgs a) {
+  __shared__ int red[2][kNT / 64];
+  const int b = blockIdx.x, tid = threadIdx.x;
+  const int2 d = a.drop[b];
+  if (d.y == 0) return;
+  const int32_t* from = a.old_table + (int64_t)b * a.old_max;
+  int first = INT32_MAX, last = -1;
+  for (int j = d.x + tid; j < d.x + d.y; j += kNT) {
+    const int page = from[j];
+    if (in_pool(a, page) && now(&a.shares[page]) < 0) {
+      atomicMin(&a.shares[page], kMark + b);
+      first = min(first, j);
+      last = max(last, j);
+    }
+  }
+  first = lowest<kNT>(first, red[0]);
+  last = -lowest<kNT>(-last, red[1]);
+  if (tid == 0) a.drop[b] = last < 0 ? int2{0, 0} : int2{first, last - first + 1};
+}
+
 constexpr int kFT = 1024;                // threads, and requests looked at together
 constexpr int kFW = kFT / 64;
 
@@ -138,14 +166,13 @@ __device__ __forceinline__ int block_sum(int x, int* red, int& total) {
 // Bound by latency, dependent loads and barriers: what there is nothing of is left out, a
 // thread asks for kEach entries in a row together, and what it has found of them, and of
 // its new request, stays in registers where all fits (the usual case).
-// ROWS: the requests as well, a wavefront each.
+// ROWS: the requests as well, a wavefront each.  MARKED: remap_mark_kernel was before.
 constexpr int kEach = 8;
 constexpr int kTurn = kFT * kEach;
-template <bool ROWS>
+template <bool ROWS, bool MARKED>
 __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
   __shared__ int s_first[kFT], s_from[kFT];
   __shared__ int red[kFW];
-  constexpr int kMark = INT32_MIN / 2;   // (a request's number is added)
   const int tid = threadIdx.x;
   const int chunks = (a.old_batch + kFT - 1) / kFT;
   const int32_t head = *a.free_head;
@@ -223,15 +250,15 @@ __global__ __launch_bounds__(kFT) void remap_finish_kernel(RemapArgs a) {
     freed += total;
   };
   int total = 0;
-  for (int c = 0; c < chunks; ++c) {
+  for (int c = 0; !MARKED && c < chunks; ++c) {
     total = open(c);
     for (int t = 0; t * kTurn < total; ++t) get(c, t, total), mark();
     __syncthreads();
   }
   for (int c = chunks - 1; c >= 0; --c) {
-    if (c < chunks - 1) total = open(c);
+    if (MARKED || c < chunks - 1) total = open(c);
     for (int t = (total + kTurn - 1) / kTurn - 1; t >= 0; --t) {
-      if (chunks > 1 || total > kTurn) get(c, t, total);
+      if (MARKED || chunks > 1 || total > kTurn) get(c, t, total);
       put();
     }
     __syncthreads();
@@ -484,6 +511,18 @@ bool remap_in_one(const RemapArgs& a) {
          (int64_t)(a.old_batch + a.new_batch) * std::max(a.old_max, a.new_max) <= kInOneEntries;
 }
 
+// Whether the marks get a launch of their own, which costs 3 us where little is dropped.
+// How much is, only the device knows: requests end where the batch shrinks, and may
+// where it does not (a beam's).  (There and back in a graph, without and with it: 64
+// requests by 4 over 31 pages, 8 000 entries to drop from, 21 us and 23; over 50, 13 000,
+// 33 and 16; over 250, 64 000, 102 and 19; by 8, 224 and 26.  25 600 entries of which none
+// is dropped 11.1 and 14.3; all 84 and 56.)
+constexpr int64_t kMarkShrinking = 12288, kMarkAny = 65536;
+bool remap_marks(const RemapArgs& a) {
+  return (int64_t)a.old_batch * a.old_max >=
+         (a.new_batch < a.old_batch ? kMarkShrinking : kMarkAny);
+}
+
 struct RemapWs {
   size_t drop, bytes;
 };
@@ -561,13 +600,20 @@ extern "C" plora_status plora_kv_remap(const plora_kv_batch* old_batch, const in
   a.last = reinterpret_cast<int2*>(pool->scratch);
   clear_error();
   if (remap_in_one(a)) {
-    hipLaunchKernelGGL(remap_finish_kernel<true>, dim3(1), dim3(kFT), 0, stream, a);
+    hipLaunchKernelGGL((remap_finish_kernel<true, false>), dim3(1), dim3(kFT), 0, stream, a);
     return launch_status();
   }
   hipLaunchKernelGGL(remap_rows_kernel, dim3(o.batch + n.batch), dim3(kNT), 0, stream, a);
-  const plora_status st = launch_status();
+  plora_status st = launch_status();
   if (st != PLORA_OK) return st;
-  hipLaunchKernelGGL(remap_finish_kernel<false>, dim3(1), dim3(kFT), 0, stream, a);
+  if (!remap_marks(a)) {
+    hipLaunchKernelGGL((remap_finish_kernel<false, false>), dim3(1), dim3(kFT), 0, stream, a);
+    return launch_status();
+  }
+  hipLaunchKernelGGL(remap_mark_kernel, dim3(o.batch), dim3(kNT), 0, stream, a);
+  st = launch_status();
+  if (st != PLORA_OK) return st;
+  hipLaunchKernelGGL((remap_finish_kernel<false, true>), dim3(1), dim3(kFT), 0, stream, a);
   return launch_status();
 }
 

@@ -164,9 +164,25 @@ def test_odd_lengths_and_pages(K):
 def test_many_pages_come_free(K):
     """More entries than are looked at together, over more requests than that."""
     rng = np.random.default_rng(11)
-    for B, most in ((40, 200), (1500, 4), (2100, 2)):
+    for B, most in ((40, 200), (1500, 4), (2100, 2), (70, 300), (1300, 60)):
         table, lens, shares, free, head = fresh(B, most, 16, rng, lead=B * most, spare=3000)
         check_remap(K, table, lens, rng.integers(0, B, B // 3), None, 16, shares, free, head)
+
+
+@pytest.mark.parametrize("grow", [False, True])
+def test_long_shared_rows_are_dropped(K, grow):
+    """Continuations of long requests, most of which end in the next remap while others go
+    on with their pages; some pages are dropped by several and held by none."""
+    rng, page, most, B = np.random.default_rng(17), 16, 700, 24
+    lens = rng.integers(page * 300, page * most, B)
+    table, lens, shares, free, head = fresh(B, most, page, rng, lens=lens, spare=400,
+                                            lead=B * most)
+    src = np.repeat(np.arange(B), 5)
+    table, lens, shares, free, head, _ = check_remap(K, table, lens, src, None, page, shares, free,
+                                                     head)
+    on = rng.choice(len(src), 160 if grow else 20)
+    keep = rng.integers(0, page * most, len(on))
+    check_remap(K, table, lens, on, keep, page, shares, free, head)
 
 
 # ---- copies and compaction ------------------------------------------------------------
