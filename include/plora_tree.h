@@ -83,9 +83,11 @@ plora_status plora_attn_tree(const void* q, int64_t q_token, int64_t q_head,
  * one drawn from its distribution: the kept tokens then have that distribution); both
  * of token_bytes 4 or 8, any values.  The first given_b nodes (given int32 [batch], or
  * NULL for 1 each; at most n_b) are certain: the root, which the step before chose, or
- * the tokens of a prompt.  They are the path's start; from its last node on, the path
- * goes to the child whose token is the node's target, of several to the one with the
- * lowest number, until there is none (from a request without given nodes: to no node).
+ * the tokens of a prompt.  Those of them that are not cut are the path's start; from its
+ * last node on, the path goes to the child whose token is the node's target, of several
+ * to the one with the lowest number, until there is none (without a start: to no node).
+ * Of a request whose nodes are all cut, as those of a tree of too many, nothing is kept:
+ * count is 0 and kv_len what it was before the step.
  *
  *   path   [T]      row q_start_b + i: the number of the path's i-th node, -1 behind
  *   count  [batch]  nodes on the path

@@ -98,7 +98,8 @@ def accept(parent, drafted, target, given, q_start, kv_len, req, T):
         at = rows(q_start, req, b)
         par = [int(parent[t]) for t in at]
         n, way = len(par), paths(par)
-        nodes = list(range(min(max(int(given[b]) if given is not None else 1, 0), n)))
+        certain = min(max(int(given[b]) if given is not None else 1, 0), n)
+        nodes = [i for i in range(certain) if way[i] is not None]
         while nodes:
             cur = nodes[-1]
             fits = [c for c in range(n) if way[c] is not None and par[c] == cur

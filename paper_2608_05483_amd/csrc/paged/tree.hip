@@ -168,26 +168,37 @@ __global__ __launch_bounds__(kNT) void tree_accept_kernel(AcceptArgs a) {
     }
   }
   if (x.there) {
-    count = min(max(given, 0), x.n);
-    for (int i = lane; i < count; i += 64) path[i] = i;
-    // nodes are cut if there are too many, and no path goes on from a cut node: one of
-    // the given ones, whose ancestors are all among them
-    bool going = count > 0;
-    if (going && x.n > kMost) {
+    const int certain = min(max(given, 0), x.n);
+    bool some = certain > 0;
+    if (some && x.n > kMost) {           // too many nodes: all are cut
       bool chain = true;
       for (int i = lane; i < x.n; i += 64) chain = chain && par[i] == i - 1;
-      going = __all(chain);
+      some = __all(chain);
     }
-    if (going) {
-      bool fine = true;
-      for (int i = lane; i < count; i += 64) fine = fine && par[i] >= -1 && par[i] < i;
-      if (!__all(fine)) {
-        int p = count - 1, q = par[p];
-        while (q >= 0 && q < p) p = q, q = par[p];
-        going = q == -1;
+    bool fine = true;
+    for (int i = lane; some && i < certain; i += 64) fine = fine && par[i] >= -1 && par[i] < i;
+    int cur = -1;
+    if (some && __all(fine)) {
+      for (int i = lane; i < certain; i += 64) path[i] = i;
+      count = certain;
+      cur = certain - 1;
+    } else if (some) {                   // the given nodes that are not cut
+      for (int i0 = 0; i0 < certain; i0 += 64) {
+        const int i = i0 + lane;
+        bool in = false;
+        if (i < certain) {
+          int p = i, q = par[p];
+          while (q >= 0 && q < p) p = q, q = par[p];
+          in = q == -1;
+        }
+        const uint64_t kept = __ballot(in);
+        if (in) path[count + __popcll(kept & ((1ull << lane) - 1))] = i;
+        if (kept) cur = i0 + 63 - __builtin_clzll(kept);
+        count += __popcll(kept);
       }
     }
-    int cur = count - 1;
+    // (a child of a node that is not cut is not cut)
+    bool going = count > 0;
     const auto target_of = [&](int i) {
       if (!hold) return target[i];
       Tok t = ht[0];

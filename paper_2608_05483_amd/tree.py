@@ -117,7 +117,8 @@ def attn_tree(q, cache: KVCache, step: Step, plan: AttnPlan, tree: Tree, scale: 
 def tree_accept(parent, drafted, target, step: Step, accepted: Accepted, given=None,
                 stream=None) -> None:
     """drafted, target [T], of accepted's type; given int32 [batch]: how many of a
-    request's first nodes are certain (None: the first)."""
+    request's first nodes are certain (None: the first).  Cut nodes are not accepted, the
+    given ones no more than others."""
     dev, dt, T = step.dev, accepted.dtype, step.T
     if accepted.dev != dev:
         _on("accepted", accepted.path, dev)
