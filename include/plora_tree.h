@@ -66,10 +66,8 @@ plora_status plora_tree_plan(const int32_t* parent, const plora_kv_step* step,
  * As plora_attn_paged, with the same plan (plora_attn_plan, made for the same step and
  * shape, groups with shared prefixes included), but a new token sees, beside the
  * request's keys before past, the new keys of its ancestors and its own, and no other
- * new key.  A chain that shares no prefix has plora_attn_paged's outputs to the bit.
- * The weights enter the product with v as there, except over a prefix that only requests
- * of more than 16 query rows per key head share: as one value of the type, as over
- * those requests' own keys, and not as two.
+ * new key.  The weights enter the product with v as there, and a chain, with or without a
+ * shared prefix, has plora_attn_paged's outputs to the bit.
  */
 plora_status plora_attn_tree(const void* q, int64_t q_token, int64_t q_head,
                              const plora_kv_cache* cache, const plora_kv_step* step,

@@ -855,8 +855,7 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   Item it = first;
   if (all_few != 0)
     it = tile ? a.tile[item] : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
-  // (attn_paged keeps two values over every prefix)
-  if (tile && (TREE ? it.gathered == 1 : it.gathered != 0))
+  if (tile && it.gathered)
     tile_item<Ty, D, true, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1,
                                 reinterpret_cast<int*>(s_n0), reinterpret_cast<int*>(s_n1));
   else if (tile)

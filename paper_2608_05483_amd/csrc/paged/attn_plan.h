@@ -36,7 +36,7 @@ struct Item {
   int32_t req;        // the request whose table row names the pages
   int32_t lo, hi;     // keys
   int32_t part;       // first row of the item's partials, -1: writes the output
-  int32_t gathered;   // tok indexes order: 1, and 2 where no member has few rows
+  int32_t gathered;   // tok indexes order
 };
 static_assert(sizeof(Item) == 32, "two 16-byte loads");
 

@@ -34,8 +34,7 @@ struct Kept {
   // entries of perm: tokens of members before it
   int32_t* moff;
   // groups: first entry of perm, keys of the prefix, who could share (then the
-  // prefix's first partial row), whether one of those has few rows (then its pieces),
-  // its first member
+  // prefix's first partial row), its pieces, its first member
   int32_t *begin, *pre, *part, *splits, *req;
 };
 static_assert(sizeof(Kept) == kKeptArrays * sizeof(int32_t*), "");
@@ -211,7 +210,6 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
       if (g >= 0 && g < a.n_groups) u = min((int64_t)a.prefix_len[g], a.max_keys);
       y.pre[i] = u <= 0 ? 0 : (int)(u & -(int64_t)a.page_size);
       y.part[i] = 0;
-      y.splits[i] = 0;
       y.req[i] = INT32_MAX;
     }
     __syncthreads();
@@ -231,7 +229,6 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
         y.u[b] = u;
         atomicAdd(&y.part[s], 1);
         atomicMin(&y.req[s], b);
-        if ((int64_t)n * a.r <= kFew) atomicOr(&y.splits[s], 1);
       }
     }
     __syncthreads();
@@ -370,7 +367,7 @@ __global__ __launch_bounds__(kNT) void attn_plan_kernel(PlanArgs a) {
     } else if (i < n_sets) {
       members(i, x.tok);
       x.hi = y.pre[i];
-      x.gathered = y.splits[i] ? 1 : 2;
+      x.gathered = 1;
       x.req = y.req[i];
     }
     int64_t items = 0, part = 0;
