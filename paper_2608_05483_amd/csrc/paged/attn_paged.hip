@@ -37,7 +37,7 @@ struct AttnArgs {
   const PlanHeader* head;
   const Item *few, *last_few, *tile;
   const ReqInfo* info;
-  int32_t batch, T, r, kv_heads, tile_cap;
+  int32_t batch, T, r, kv_heads;
   float c;                  // |scale| log2(e)
   uint32_t flip;            // sign bits for q where scale < 0
   uint16_t* out;
@@ -837,8 +837,6 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   __shared__ FewShared sh;
   static_assert(sizeof(s_k0) == 2 * kFew * D * sizeof(float), "two wavefronts' outputs");
   const uint32_t turn = blockIdx.x >> 3, in = blockIdx.x & 7;
-  // (the item of a step without few items, read beside their number)
-  const Item first = a.tile[min(blockIdx.x / (uint32_t)a.kv_heads, (uint32_t)a.tile_cap - 1)];
   const int few = a.head->few, all_few = few + a.head->later;
   const uint32_t tiles = ((uint32_t)a.head->tiles * a.kv_heads + 7) / 8;
   const uint32_t fews = ((uint32_t)all_few * a.kv_heads + 7) / 8;
@@ -852,9 +850,8 @@ __global__ __launch_bounds__(kNT, D == 64 ? 3 : 2) void items_kernel(AttnArgs a)
   const int kvh = index % a.kv_heads;
   // (the work groups behind the last item would pass the lists' ends)
   if (item >= (uint32_t)(tile ? a.head->tiles : all_few)) return;
-  Item it = first;
-  if (all_few != 0)
-    it = tile ? a.tile[item] : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
+  const Item it = tile ? a.tile[item]
+                       : (int)item < few ? a.few[item] : a.last_few[few - (int)item];
   if (tile && it.gathered)
     tile_item<Ty, D, true, TREE>(a, it, kvh, sh.most, s_k0, s_k1, s_v0, s_v1,
                                 reinterpret_cast<int*>(s_n0), reinterpret_cast<int*>(s_n1));
@@ -1133,7 +1130,6 @@ plora_status attend(const void* q, int64_t q_token, int64_t q_head, const plora_
   a.tile = reinterpret_cast<const Item*>(p + l.tile);
   a.order = reinterpret_cast<const int32_t*>(p + l.order);
   a.info = reinterpret_cast<const ReqInfo*>(p + l.req);
-  a.tile_cap = b.tile_cap;
   a.batch = s.batch;
   a.T = s.T;
   a.r = b.r;
